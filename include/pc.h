@@ -55,6 +55,13 @@ typedef enum {
 #define PC_MAX_FREQ 2048u          /* largest exact frequency / request-count bin */
 #define PC_FREQ_CLASSES 32u        /* frequency classes floor(log2 f) */
 #define PC_MAX_FOOTPRINT (1u << 24) /* largest exact footprint bin */
+#define PC_BF16 0u                 /* element types of a paged cache and its new tokens */
+#define PC_F16 1u
+#define PC_FP8_E4M3 2u             /* 8 bits: 4 of exponent, 3 of fraction, no infinity */
+#define PC_MAX_PAGE 65536u         /* largest page of a paged cache, in slots */
+#define PC_MAX_HEADS 1024u         /* largest number of query heads */
+#define PC_MAX_HEAD_DIM 256u
+#define PC_ATTN_CAUSAL 1u          /* pc_attn_paged flag */
 
 /* Human-readable name of a status code (static storage). */
 const char *pc_status_string(pc_status s);
@@ -463,6 +470,115 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
                     size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * A paged cache of KV blocks: the blocks that the keys above name, and that
+ * the eviction scored above would drop (Sec. 2.2: the server keeps the keys
+ * and values of every token of a block, and a request whose prefix is cached
+ * computes only its new tokens).
+ *
+ * A page holds page_size slots for each of n_kv_heads heads.  Entry d of head h
+ * in slot o of page p is at element
+ *     p * stride_page + h * stride_head + o * stride_slot + d
+ * of k (and of v), d < head_dim; distinct entries lie apart.  Slot j of
+ * sequence s is in page page_table[s * table_stride + j / page_size].  A page
+ * may stand in the tables of many sequences (a shared prefix).
+ *
+ *   dtype       PC_BF16, PC_F16, or PC_FP8_E4M3, whose values are the codes
+ *               times a scale per head (k_scale, v_scale: float[n_kv_heads];
+ *               NULL for the other types)
+ *   head_dim    a multiple of 16, at most PC_MAX_HEAD_DIM
+ *   k, v and the strides in bytes are multiples of 16
+ *
+ * Calls on it take new tokens as chunks: rows q_off[s] .. q_off[s+1] - 1 of the
+ * token arrays are sequence s's newest ones (uint32[n_seqs + 1], non-decreasing,
+ * q_off[0] = 0, q_off[n_seqs] = the number of rows; none is fine), and kv_len[s] (uint32[n_seqs])
+ * is its length with them: row i of the chunk has slot kv_len[s] - rows + i.
+ * Lengths of zero are fine; no kv_len may exceed max_kv, the slots that a
+ * row of page_table has room for or fewer.  Rows whose slot is negative, table
+ * entries of n_pages or more that a call needs, lengths above max_kv and an
+ * invalid q_off set the workspace status to 2; nothing is read or written out
+ * of bounds.  Table entries past a sequence's length are not read.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    void *k, *v;
+    const float *k_scale, *v_scale;
+    uint64_t stride_page, stride_head, stride_slot; /* elements */
+    uint32_t dtype;
+    uint32_t n_pages, page_size, n_kv_heads, head_dim;
+} pc_kv_cache;
+
+/* New tokens' keys and values into their slots.
+ *   k, v     new rows of `dtype` (PC_BF16 or PC_F16; the cache has the same type or
+ *            PC_FP8_E4M3): head h of row t at element t * stride_row + h *
+ *            stride_head, head_dim contiguous; pointers and strides in bytes
+ *            multiples of 16.  An 8-bit cache takes x / scale, at most 448 in
+ *            magnitude, rounded to the nearest code, ties to even; NaN stays NaN.
+ * A row without a slot or page is left out (status 2).  Two rows that share a
+ * slot (a page in two tables) leave it unspecified. */
+size_t pc_kv_append_ws(void);
+pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                       const uint32_t *kv_len, const uint32_t *q_off, uint32_t n_seqs, uint32_t n_rows,
+                       uint32_t max_kv, const void *k, uint64_t k_stride_row, uint64_t k_stride_head,
+                       const void *v, uint64_t v_stride_row, uint64_t v_stride_head, uint32_t dtype, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* Attention of new tokens over the cache (which holds them already).
+ *     slots a row at position x sees: j < kv_len[s], j <= x if PC_ATTN_CAUSAL,
+ *                                     j > x - window if window > 0
+ *     s_j = scale * <q, k_j>    lse = log sum_j exp(s_j)
+ *     out = sum_j exp(s_j - lse) v_j
+ *     weight_out[s][h][j] = weight[s][h][j] + sum over the chunk's rows and the
+ *                           heads that share h of exp(s_j - lse)
+ * Query head e reads key/value head e / (n_heads / n_kv_heads).  A row that sees
+ * nothing has out = 0 and lse = -infinity and adds no weight.  What a row does not
+ * see never reaches its outputs, whatever its values.
+ *
+ *   q, out     `dtype` PC_BF16 or PC_F16 (the cache the same or PC_FP8_E4M3), head e of
+ *              row t at element t * stride_row + e * stride_head; pointers and
+ *              strides in bytes multiples of 16
+ *   max_q      no sequence has more new rows (more set status 2, and what is past
+ *              max_q may be left out); with max_q * group at most 32 the
+ *              call takes the path for few rows
+ *   lse        float[n_rows * n_heads] or NULL
+ *   weight     float, [s][h] rows of max_kv entries, weight_stride apart (s * n_kv_heads + h
+ *              times weight_stride), or NULL: zeros; entries from kv_len on count as 0
+ *   weight_out the same layout, or NULL: no weights; may be weight.  All max_kv
+ *              entries are written, 0 from kv_len on.
+ *   n_heads    a multiple of n_kv_heads; scale finite
+ * Scores, statistics and sums are in 32 bits; exp(s_j - max) is rounded to `dtype`
+ * for its product with v.  Results do not depend on timing (no atomics). */
+size_t pc_attn_paged_ws(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32_t max_kv, uint32_t n_heads,
+                        uint32_t n_kv_heads, uint32_t head_dim, int with_weight);
+pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                        const uint32_t *kv_len, const uint32_t *q_off, uint32_t n_seqs, uint32_t n_rows,
+                        uint32_t max_q, uint32_t max_kv, const void *q, uint64_t q_stride_row,
+                        uint64_t q_stride_head, uint32_t dtype, uint32_t n_heads, float scale, uint32_t flags,
+                        uint32_t window, void *out, uint64_t out_stride_row, uint64_t out_stride_head, float *lse,
+                        const float *weight, float *weight_out, uint64_t weight_stride, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/* Eviction by accumulated attention weight, the token-level counterpart of the
+ * block policies above: every (sequence, head) keeps min(kv_len, budget) slots.
+ * The last min(recent, that) stay; the rest of the places go to the largest
+ * weights (equal ones: the lowest slot first; NaN is above infinity), in slot
+ * order.  Kept slot number r moves to slot r of the destination table's row.
+ *
+ *   weight     as in pc_attn_paged
+ *   budget     1 ..; recent at most budget
+ *   kept       uint32, [s][h] rows of `budget` entries: the slots kept, PC_NONE behind them
+ *   weight_out float, the same layout: their weights, 0 behind them, or NULL
+ *   new_len    uint32[n_seqs]: min(kv_len, budget)
+ *   dst_table  uint32, [s] rows dst_stride apart of pages with room for `budget` slots, in the
+ *              same cache, none of them a page of any of the call's sequences (shared
+ *              prefix pages are never written); NULL: nothing is moved
+ * With max_kv above 2^31 - 2^16 the call returns PC_ERR_TOO_LARGE. */
+size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv);
+pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                      const uint32_t *kv_len, uint32_t n_seqs, uint32_t max_kv, const float *weight,
+                      uint64_t weight_stride, uint32_t budget, uint32_t recent, const uint32_t *dst_table,
+                      uint64_t dst_stride, uint32_t *kept, float *weight_out, uint32_t *new_len, void *ws,
+                      size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Device-side status.  Every call clears word 0 of its workspace; kernels
  * record a non-zero code there instead of faulting or hanging:
  *   1  a wait on another workgroup (decoupled look-back) gave up after a
@@ -470,7 +586,7 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
  *   2  a bad layout: pc_hash_blocks, a request's tokens or blocks fall
  *      outside the arrays (that request was skipped); the calls that take a
  *      request table, a table that is not a non-decreasing prefix ending at
- *      n; pc_stack_distance, prev / next that are not mutual links (outputs
+ *      n; the calls on a paged cache, a length, page or row that does not fit; pc_stack_distance, prev / next that are not mutual links (outputs
  *      undefined, nothing written out of bounds);
  *   3  pc_mrc_weighted and the profiles: edges not non-decreasing (bins
  *      undefined);

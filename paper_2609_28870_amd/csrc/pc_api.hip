@@ -46,6 +46,13 @@ static const char *kernel_name(KernelId k) {
     case K_RUNS_FILL: return "runs_fill";
     case K_BELADY_RANK: return "belady_rank";
     case K_BELADY: return "belady";
+    case K_KV_APPEND: return "kv_append";
+    case K_KV_EVICT_SELECT: return "kv_evict_select";
+    case K_KV_EVICT_MOVE: return "kv_evict_move";
+    case K_ATTN_ROWS: return "attn_rows";
+    case K_ATTN_CHUNK: return "attn_chunk";
+    case K_ATTN_JOIN: return "attn_join";
+    case K_ATTN_WEIGHT: return "attn_weight";
     case K_MRC_MAP: return "mrc_map";
     case K_COUNT: break;
     }

@@ -1,0 +1,361 @@
+// The pieces that the attention kernels over the paged cache share: matrix
+// products, the work list, tiles of keys and values.  Not part of the ABI.
+#pragma once
+
+#include "pc_kv.h"
+
+namespace pc {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float MINUS_INF = -__builtin_inff();
+
+struct Bf16 {
+    // exp2(score - max) is at most 1
+    static constexpr float TOP = 0.f;
+    static __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        const bf16x2 v = {(__bf16)x, (__bf16)y};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+    template <bool HI>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+    }
+    static constexpr uint32_t SIGNS = 0x80008000u, EXPONENT = 0x7F80u;
+    static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
+};
+struct F16 {
+    // f16 has five exponent bits: weights down to 2^-29 of the largest stay
+    // normal numbers when that one is 2^15 (the factor cancels in sum p v / sum p)
+    static constexpr float TOP = 15.f;
+    static __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        const f16x2 v = {(_Float16)x, (_Float16)y};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+    template <bool HI>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
+    }
+    static constexpr uint32_t SIGNS = 0x80008000u, EXPONENT = 0x7C00u;
+    static __device__ __forceinline__ float value(uint32_t bits) {
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    }
+};
+
+// sixteen 8-bit codes as two pieces of eight elements
+template <class T>
+__device__ __forceinline__ void expand(uint4 x, uint4 *lo, uint4 *hi) {
+    *lo = make_uint4(T::template from_e4m3<false>(x.x), T::template from_e4m3<true>(x.x),
+                     T::template from_e4m3<false>(x.y), T::template from_e4m3<true>(x.y));
+    *hi = make_uint4(T::template from_e4m3<false>(x.z), T::template from_e4m3<true>(x.z),
+                     T::template from_e4m3<false>(x.w), T::template from_e4m3<true>(x.w));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// the same lane of the other half of the wave
+__device__ __forceinline__ void both_halves(float x, float *lower, float *upper) {
+    const uint32_t b = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    *lower = __uint_as_float(r[0]);
+    *upper = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_of_halves(float x) {
+    float a, b;
+    both_halves(x, &a, &b);
+    return fmaxf(a, b);
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+    float a, b;
+    both_halves(x, &a, &b);
+    return a + b;
+}
+
+// Keys and values of 16-bit elements lie in LDS as rows of D, in pieces of 16
+// bytes.  A wave reads a column of pieces over consecutive rows (keys) and the
+// same four pieces of four consecutive rows (the transposed reads of values);
+// piece c of row k is at c ^ spread(k), so that both, and writes of whole rows,
+// meet every bank once.
+template <int D>
+__device__ __forceinline__ uint32_t spread(uint32_t row) {
+    return ((row & 3) << 1 | (row >> 2 & 1)) & (D / 8 - 1);
+}
+template <int D>
+__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
+    return row * (D * 2) + ((c ^ spread<D>(row)) * 16);
+}
+// four keys of one value dimension a lane: rows row .. row + 3 of the 16 lanes
+// of each group, dimension 16 * (group & 1) + lane % 16 of the 32 from d0
+template <int D>
+__device__ __forceinline__ uint2 read_transposed(const char *tile, uint32_t row, uint32_t d) {
+    // this lane's address: row and d are those of the four elements that it fetches
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const char *p = tile + piece_at<D>(row, d / 8) + (d % 8) * 2;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
+}
+
+// ------------------------------------------------------------------ arguments
+
+struct AttnArgs {
+    KvView kv;
+    const uint32_t *table, *kv_len, *q_off;
+    uint64_t table_stride;
+    uint32_t n_seqs, n_rows, max_q, max_kv;
+    const char *q;               // strides in bytes
+    char *out;
+    uint64_t q_row, q_head, o_row, o_head;
+    float *lse;                  // user's, or nullptr
+    const float *weight;
+    float *weight_out;
+    uint64_t weight_stride;
+    uint32_t n_heads, group;
+    FastDiv by_group;
+    float scale;
+    uint32_t causal, window;
+    // the work list
+    uint32_t target;             // items wanted
+    uint32_t least;              // tiles of an item, at least
+    uint32_t row_tile, key_tile; // rows, keys
+    uint32_t slots;              // partial results that fit
+    uint32_t slot_rows;
+    // workspace
+    int32_t *status;
+    float *part;                 // [slot][row][padded dim]
+    float2 *part_ml;             // [slot][row] maximum (base 2), sum
+    float *lse2;                 // [row][head] base 2, for the weights
+    float *scores;               // [seq][kv head][row][score_stride] base 2 (few rows, with weights)
+    uint64_t score_stride;
+    float *weight_part;          // [row part][seq][kv head][max_kv]
+    uint32_t weight_parts;
+};
+
+// Keys that rows i0 .. i1 of a sequence see between them: [lo, hi).
+struct Range {
+    uint32_t lo, hi;
+};
+__device__ __forceinline__ Range seen(const AttnArgs &a, const Seq &q, uint32_t i0, uint32_t i1) {
+    const int64_t j0 = (int64_t)q.len - q.rows;
+    int64_t hi = a.causal ? j0 + i1 + 1 : (int64_t)q.len, lo = a.window ? j0 + i0 - (int64_t)a.window + 1 : 0;
+    if (hi > (int64_t)q.len) hi = q.len;
+    if (lo < 0) lo = 0;
+    if (hi < lo) hi = lo;
+    return Range{(uint32_t)lo, (uint32_t)hi};
+}
+// slots that row i sees: first .. last (none if last < first)
+__device__ __forceinline__ void seen_by_row(const AttnArgs &a, const Seq &q, uint32_t i, int32_t *first, int32_t *last) {
+    const int64_t x = (int64_t)q.len - q.rows + i;
+    const int64_t lo = a.window ? x - (int64_t)a.window + 1 : 0;
+    *first = lo > 0 ? (lo < 0x7FFFFFFF ? (int32_t)lo : 0x7FFFFFFF) : 0;
+    *last = a.causal && x < (int64_t)q.len ? (x < 0 ? -1 : (int32_t)x) : (int32_t)q.len - 1;
+}
+
+// ------------------------------------------------------------------ work list
+// An item is a tile of rows (a row is a token and one of the query heads that
+// share a key/value head) against a range of key tiles.  Every workgroup works
+// the list out from the lengths, which only the device knows: the tiles of
+// all sequences divided by the items wanted give the length of a range, so that a
+// few long sequences fill the chip as well as many short ones.
+struct Shape {   // one sequence's part of the list
+    Seq q;
+    Range keys;
+    uint32_t row_tiles, key_tiles;
+};
+__device__ __forceinline__ Shape shape_of(const AttnArgs &a, uint32_t s) {
+    Shape h;
+    bool bad;
+    h.q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
+    if (h.q.rows > a.max_q) h.q.rows = a.max_q;
+    h.keys = h.q.rows ? seen(a, h.q, 0, h.q.rows - 1) : Range{0, 0};
+    h.keys.lo &= ~(a.key_tile - 1);   // a power of two
+    h.row_tiles = (uint32_t)(((uint64_t)h.q.rows * a.group + a.row_tile - 1) / a.row_tile);
+    h.key_tiles = (h.keys.hi - h.keys.lo + a.key_tile - 1) / a.key_tile;
+    return h;
+}
+struct Item {
+    uint32_t seq, head, row_tile, split;
+    uint32_t splits, length;   // ranges of the sequence, tiles in each
+    uint32_t slot;             // of the partial result (splits > 1)
+    Shape shape;
+    bool there;
+};
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+
+// by_seq: the sequence `key` as a whole (slot: its first); else item number `key`
+__device__ __forceinline__ Item find_item(const AttnArgs &a, bool by_seq, uint32_t key) {
+    const int lane = threadIdx.x & (WAVE - 1);
+    Item it;
+    it.there = false;
+    uint64_t tiles = 0;
+    Shape h;
+    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
+        if (s0 + lane < a.n_seqs) {
+            h = shape_of(a, s0 + lane);
+            tiles += (uint64_t)h.row_tiles * h.key_tiles;
+        }
+    }
+#pragma unroll
+    for (int step = 1; step < WAVE; step *= 2) tiles += __shfl_xor((unsigned long long)tiles, step, WAVE);
+    const uint64_t len = (tiles * a.kv.n_kv + a.target - 1) / a.target;
+    it.length = uniform(len > a.least ? (uint32_t)(len < 0x7FFFFFFFu ? len : 0x7FFFFFFFu) : a.least);
+    uint64_t base = 0, slot = 0;
+    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
+        const uint32_t s = s0 + lane;
+        uint32_t items = 0, splits = 1;
+        if (s < a.n_seqs) {
+            if (a.n_seqs > WAVE) h = shape_of(a, s);
+            splits = (h.key_tiles + it.length - 1) / it.length;
+            splits = splits ? splits : 1;
+            const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
+            items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
+        }
+        const uint32_t end = wave_incl_scan(items), partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
+        int at;
+        if (by_seq) {
+            at = key >= s0 && key - s0 < WAVE ? (int)(key - s0) : WAVE;
+        } else {
+            at = __popcll(ballot(base + end <= key));
+        }
+        at = (int)uniform((uint32_t)at);
+        if (at < WAVE) {
+            it.there = true;
+            it.seq = s0 + at;
+            it.splits = from_lane(splits, at);
+            it.shape.q.first = from_lane(h.q.first, at);
+            it.shape.q.rows = from_lane(h.q.rows, at);
+            it.shape.q.len = from_lane(h.q.len, at);
+            it.shape.keys.lo = from_lane(h.keys.lo, at);
+            it.shape.keys.hi = from_lane(h.keys.hi, at);
+            it.shape.row_tiles = from_lane(h.row_tiles, at);
+            it.shape.key_tiles = from_lane(h.key_tiles, at);
+            it.slot = (uint32_t)slot + from_lane(slot_end - partial, at);
+            it.head = it.row_tile = it.split = 0;
+            if (!by_seq) {
+                // heads first (neighbouring workgroups are on different XCDs, so with 2, 4 or 8
+                // heads an L2 holds one or few heads' keys), then rows, the last ones first
+                // (they see the most keys), then ranges
+                const uint32_t i = key - (uint32_t)(base + from_lane(end - items, at));
+                it.slot += i;
+                it.head = i % a.kv.n_kv;
+                const uint32_t j = i / a.kv.n_kv;
+                it.row_tile = it.shape.row_tiles - 1 - j % it.shape.row_tiles;
+                it.split = j / it.shape.row_tiles;
+            }
+            return it;
+        }
+        base += from_lane(end, WAVE - 1);
+        slot += from_lane(slot_end, WAVE - 1);
+    }
+    return it;
+}
+// slot of an item of a sequence found by_seq
+__device__ __forceinline__ uint32_t slot_of(const AttnArgs &a, const Item &it, uint32_t head, uint32_t row_tile, uint32_t split) {
+    return it.slot + (split * it.shape.row_tiles + (it.shape.row_tiles - 1 - row_tile)) * a.kv.n_kv + head;
+}
+
+// ------------------------------------------------------------------ rows
+
+// A row's query as the right operand of scores^T = K Q^T: step s holds dimensions
+// 32 (s / 2) + 16 half + 8 (s % 2) .. + 7, the order in which keys are read, too
+// (the sum over dimensions takes any order that both operands share).
+constexpr __device__ __forceinline__ uint32_t dim_of_step(uint32_t step, uint32_t half) {
+    return 32 * (step / 2) + 16 * half + 8 * (step % 2);
+}
+template <int D>
+__device__ __forceinline__ void load_query(const AttnArgs &a, const char *row, bool there, uint32_t half, uint32_t flip,
+                                           bool zero, uint4 (&q)[D / 16]) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        const uint32_t d = dim_of_step(s, half);
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (there && !zero && d < a.kv.dim) {
+            x = *(const uint4 *)(row + d * 2);
+            x = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+        }
+        q[s] = x;
+    }
+}
+
+// softmax state of the rows of a wave: lane % 32 is the row; the maximum is
+// common to both halves, the sum is each half's own until the end
+template <class T, int D>
+struct Rows {
+    f32x16 o[D / 32];
+    float m, l;
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) o[b] = f32x16(0.f);
+        m = MINUS_INF;
+        l = 0.f;
+    }
+    // scores of 32 * B keys -> weights packed as the right operand of O^T += V^T P^T
+    template <int B>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[B], float c, uint4 (&p)[2 * B]) {
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = max_of_halves(top);
+        const float next = fmaxf(m, top);
+        // a row that has seen nothing yet keeps weights of 0: exp2(-inf - 0)
+        const float ref = next == MINUS_INF ? 0.f : next;
+        if (ballot(next > m)) {
+            const float f = exp2_fast((m - ref) * c);
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b) o[b] *= f;
+            m = next;
+        }
+        const float shift = T::TOP - ref * c;
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = exp2_fast(fmaf(s[b][r], c, shift));
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) sum += (s[b][r] + s[b][r + 1]) + (s[b][r + 2] + s[b][r + 3]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                p[2 * b + t] = make_uint4(T::pack(s[b][8 * t], s[b][8 * t + 1]), T::pack(s[b][8 * t + 2], s[b][8 * t + 3]),
+                                          T::pack(s[b][8 * t + 4], s[b][8 * t + 5]), T::pack(s[b][8 * t + 6], s[b][8 * t + 7]));
+        }
+        l += sum;
+    }
+    // O^T += V^T P^T over 16 keys from row k0 of the tile
+    __device__ __forceinline__ void add(const char *v, uint32_t k0, uint4 p) {
+        const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32, row = k0 + 4 * half + lane % 16 / 4;
+        const uint32_t d = (lane / 16 % 2) * 16 + (lane % 4) * 4;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            const uint2 x = read_transposed<D>(v, row, 32 * b + d), y = read_transposed<D>(v, row + 8, 32 * b + d);
+            o[b] = T::mfma(make_uint4(x.x, x.y, y.x, y.y), p, o[b]);
+        }
+    }
+};
+
+// key of score register r in its block of 32
+__device__ __forceinline__ uint32_t key_of(uint32_t r, uint32_t half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+// The factor of scores (base 2) for head h, as a positive number: its sign, or a
+// zero, goes to the queries.
+__device__ __forceinline__ float score_factor(const AttnArgs &a, uint32_t h, uint32_t *flip, bool *zero) {
+    float c = a.scale * LOG2E;
+    if (a.kv.k_scale) c *= a.kv.k_scale[h];
+    *zero = c == 0.f;
+    *flip = c < 0.f ? 0x80008000u : 0u;
+    return *zero ? 1.f : fabsf(c);
+}
+
+}  // namespace pc

@@ -1,0 +1,897 @@
+// Attention of new tokens over the paged cache (pc_attn_paged): the path for few
+// rows (decode, drafted tokens), the path for chunks, the join of partial results
+// and the accumulated weights.
+#include <math.h>
+
+#include "pc_attn.h"
+
+namespace pc {
+
+// ------------------------------------------------------------ keys and values
+
+// address of a slot's entry in `base`, the page taken as is (it is below n_pages)
+__device__ __forceinline__ uint64_t entry_at(const KvView &kv, uint32_t page, uint32_t off, uint32_t head) {
+    return page * kv.sp + off * kv.st + head * kv.sh;
+}
+// a table entry that does not fit reads page 0 (the join reports it)
+__device__ __forceinline__ uint32_t page_of(const KvView &kv, uint32_t entry) { return entry < kv.n_pages ? entry : 0; }
+
+template <class T>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+    return (w & T::EXPONENT) == T::EXPONENT || (w >> 16 & T::EXPONENT) == T::EXPONENT;
+}
+// zeroes the elements that are not finite; says whether there were any
+template <class T>
+__device__ __forceinline__ bool drop_not_finite(uint4 *x) {
+    uint32_t w[4] = {x->x, x->y, x->z, x->w};
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & T::EXPONENT) == T::EXPONENT) { w[i] &= 0xFFFF0000u; any = true; }
+        if ((w[i] >> 16 & T::EXPONENT) == T::EXPONENT) { w[i] &= 0xFFFFu; any = true; }
+    }
+    *x = make_uint4(w[0], w[1], w[2], w[3]);
+    return any;
+}
+
+// Values that are not finite, where rows differ in which keys they see: the
+// matrix product would carry 0 * inf = NaN to rows that do not see the key.  There the
+// tile was written without them, and they are added here to the rows that do.
+// Rare, so it is written for size: one key at a time.
+template <class T, bool F8, int D, int B>
+__device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const f32x16 (&p)[B], uint64_t keys, const AttnArgs &a,
+                                               uint32_t seq, uint32_t head, uint32_t k0, int32_t first, int32_t last) {
+    const uint32_t half = threadIdx.x / 32 % 2;
+    while (keys) {
+        const uint32_t i = (uint32_t)__builtin_ctzll(keys), key = k0 + i, in = i % 32, reg = in / 8 * 4 + in % 4;
+        keys &= keys - 1;
+        float mine = 0.f;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (b == (int)(i / 32) && r == (int)reg) mine = p[b][r];
+        float lower, upper;
+        both_halves(mine, &lower, &upper);
+        const float w = in / 4 % 2 ? upper : lower;
+        const bool visible = (int32_t)key >= first && (int32_t)key <= last;
+        const uint32_t at = a.kv.by_page.div(key);
+        const uint32_t page = page_of(a.kv, a.table[(uint64_t)seq * a.table_stride + at]);
+        const char *v = a.kv.v + entry_at(a.kv, page, key - at * a.kv.page, head);
+#pragma unroll 1
+        for (int b = 0; b < D / 32; ++b) {
+            f32x16 add = f32x16(0.f);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t d = 32 * b + key_of(r, half);
+                if (d < a.kv.dim) {
+                    float x;
+                    if (F8) x = T::value(T::template from_e4m3<false>(*(const uint8_t *)(v + d)) & 0xFFFF);
+                    else x = T::value(*(const uint16_t *)(v + 2 * d));
+                    if (visible && !(fabsf(x) < __builtin_inff())) add[r] = w * x;
+                }
+            }
+#pragma unroll
+            for (int bb = 0; bb < D / 32; ++bb)
+                if (bb == b) state.o[bb] += add;
+        }
+    }
+}
+
+// A row's result: whole (its sequence is one item long), or a part for the join.
+template <class T, int D>
+__device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, const f32x16 (&o)[D / 32], float m, float l,
+                                           uint32_t at, uint32_t t, uint32_t head, uint32_t half) {
+    if (it.splits > 1) {
+        if (it.slot >= a.slots) return;
+        const uint64_t row = (uint64_t)it.slot * a.slot_rows + at;
+        if (half == 0) a.part_ml[row] = make_float2(m, l);
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(float4 *)(a.part + row * D + 32 * b + key_of(r, half)) =
+                    make_float4(o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]);
+        return;
+    }
+    const float base2 = m == MINUS_INF ? MINUS_INF : m + __log2f(l) - T::TOP;
+    const float f = m == MINUS_INF ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / l;
+    if (half == 0) {
+        if (a.lse) a.lse[(uint64_t)t * a.n_heads + head] = base2 * LN2;
+        if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + head] = base2;
+    }
+    char *out = a.out + (uint64_t)t * a.o_row + head * a.o_head;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const uint32_t d = 32 * b + key_of(r, half);
+            if (d < a.kv.dim)
+                *(uint2 *)(out + 2 * d) = make_uint2(T::pack(o[b][r] * f, o[b][r + 1] * f), T::pack(o[b][r + 2] * f, o[b][r + 3] * f));
+        }
+}
+
+// ------------------------------------------------------------------ few rows
+
+// At most 32 rows (new tokens times the query heads that share a key/value head)
+// of a sequence against a range of its keys.  Bound by the bytes of keys and
+// values: a wave takes 32 keys at a time on its own (every fourth such tile of the
+// item), the next tile's bytes on their way to its registers meanwhile.  Keys
+// go straight into the matrix product, a lane per key; values pass through
+// LDS for the transposed read.  The four waves' results are joined in LDS.
+template <class T, bool F8, int D, bool WEIGHTS>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a) {
+    constexpr int PIECES = F8 ? D / 32 : D / 16;   // 16 bytes, of one lane's half of a key
+    __shared__ __attribute__((aligned(16))) char tiles[4 * 32 * D * 2];
+    __shared__ float2 join_ml[2][64];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+    const Item it = find_item(a, false, blockIdx.x);
+    if (!it.there) return;
+    const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32, wave = uniform(threadIdx.x / WAVE), col = lane % 32;
+    const Seq &sq = it.shape.q;
+    const uint32_t rows = sq.rows * a.group;
+    uint32_t flip;
+    bool zero;
+    const float c = score_factor(a, it.head, &flip, &zero);
+    // this lane's row
+    const bool valid = col < rows;
+    const uint32_t token = a.by_group.div(col), head = it.head * a.group + (col - token * a.group);
+    int32_t first = 0, last = 0x7FFFFFFF;
+    if (valid) seen_by_row(a, sq, token, &first, &last);
+    int32_t all_first = first, all_last = last;   // keys that every row sees
+#pragma unroll
+    for (int step = 1; step < 32; step *= 2) {
+        all_first = max(all_first, __shfl_xor(all_first, step, WAVE));
+        all_last = min(all_last, __shfl_xor(all_last, step, WAVE));
+    }
+    all_first = (int32_t)uniform((uint32_t)all_first);
+    all_last = (int32_t)uniform((uint32_t)all_last);
+    uint4 q[D / 16];
+    load_query<D>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
+
+    const uint32_t t_end = min(it.shape.key_tiles, (it.split + 1) * it.length);
+    uint32_t t = it.split * it.length + wave;
+    const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
+    char *tile = tiles + wave * (32 * D * 2);
+    Rows<T, D> state;
+    state.clear();
+    uint4 k[PIECES], v[PIECES];
+    uint64_t at = 0;
+    uint32_t entry = 0, off = 0;
+    auto look_up = [&](uint32_t tt) {
+        const uint32_t j = min(it.shape.keys.lo + tt * 32 + col, it.shape.keys.hi - 1), p = a.kv.by_page.div(j);
+        off = j - p * a.kv.page;
+        entry = table[p];
+    };
+    auto piece = [&](int i) {   // its offset in the entry; past the head's dimensions, the first one
+        const uint32_t o = F8 ? 32 * i + 16 * half : 2 * dim_of_step(i, half);
+        return o < a.kv.dim * (F8 ? 1 : 2) ? o : 0;
+    };
+    auto load = [&](const char *base, uint4 (&x)[PIECES]) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x[i] = *(const uint4 *)(base + at + piece(i));
+    };
+    if (t < t_end) {
+        look_up(t);
+        at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
+        load(a.kv.k, k);
+        load(a.kv.v, v);
+        if (t + 4 < t_end) look_up(t + 4);
+    }
+    for (; t < t_end; t += 4) {
+        const bool more = t + 4 < t_end;
+        const uint32_t k0 = it.shape.keys.lo + t * 32;
+        const bool full = (int32_t)k0 >= all_first && (int32_t)k0 + 31 <= all_last;
+        f32x16 s[1] = {f32x16(0.f)};
+        if (a.kv.dim != D) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if ((F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            if (F8) {
+                uint4 x, y;
+                expand<T>(k[i / 2], &x, &y);
+                s[0] = T::mfma(i % 2 ? y : x, q[i], s[0]);
+            } else {
+                s[0] = T::mfma(k[i % PIECES], q[i], s[0]);
+            }
+        }
+        if (more) {
+            at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
+            load(a.kv.k, k);
+        }
+        uint64_t odd = 0;   // keys with values that are not finite, where rows differ
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t n = F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
+            uint4 x[2] = {v[i], v[i]};
+            if (F8) expand<T>(v[i], &x[0], &x[1]);
+#pragma unroll
+            for (int e = 0; e < (F8 ? 2 : 1); ++e) {
+                if (!full) {
+                    const uint64_t b = ballot(drop_not_finite<T>(&x[e]));
+                    odd |= (b | b >> 32) & 0xFFFFFFFFull;
+                }
+                *(uint4 *)(tile + piece_at<D>(col, n + e)) = x[e];
+            }
+        }
+        if (more) {
+            load(a.kv.v, v);
+            if (t + 8 < t_end) look_up(t + 8);
+        }
+        if (!full) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int32_t key = (int32_t)(k0 + key_of(r, half));
+                if (key < first || key > last) s[0][r] = MINUS_INF;
+            }
+        }
+        if (WEIGHTS && valid) {
+            float *w = a.scores + (((uint64_t)it.seq * a.kv.n_kv + it.head) * a.slot_rows + col) * a.score_stride + k0 + 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(float4 *)(w + 2 * r) = make_float4(s[0][r] * c, s[0][r + 1] * c, s[0][r + 2] * c, s[0][r + 3] * c);
+        }
+        uint4 p[2];
+        state.template weigh<1>(s, c, p);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        state.add(tile, 0, p[0]);
+        state.add(tile, 16, p[1]);
+        __builtin_amdgcn_wave_barrier();
+        if (odd) add_not_finite<T, F8, D, 1>(state, s, odd, a, it.seq, it.head, k0, first, last);
+    }
+    float m = state.m == MINUS_INF ? MINUS_INF : state.m * c, l = sum_of_halves(state.l);
+    // waves 2 and 3 to 0 and 1, then 1 to 0
+    for (int from = 2; from >= 1; from /= 2) {
+        __syncthreads();
+        float *buf = (float *)tiles + (wave % from) * (32 * D);
+        if (wave >= (uint32_t)from && wave < 2u * from) {
+            join_ml[wave % from][lane] = make_float2(m, l);
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(float4 *)(buf + ((b * 4 + r / 4) * WAVE + lane) * 4) =
+                        make_float4(state.o[b][r], state.o[b][r + 1], state.o[b][r + 2], state.o[b][r + 3]);
+        }
+        __syncthreads();
+        if (wave < (uint32_t)from) {
+            const float2 ml = join_ml[wave][lane];
+            const float top = fmaxf(m, ml.x), ref = top == MINUS_INF ? 0.f : top;
+            const float f = exp2_fast(m - ref), g = exp2_fast(ml.x - ref);
+            m = top;
+            l = l * f + ml.y * g;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const float4 x = *(const float4 *)(buf + ((b * 4 + r / 4) * WAVE + lane) * 4);
+                    state.o[b][r] = state.o[b][r] * f + x.x * g;
+                    state.o[b][r + 1] = state.o[b][r + 1] * f + x.y * g;
+                    state.o[b][r + 2] = state.o[b][r + 2] * f + x.z * g;
+                    state.o[b][r + 3] = state.o[b][r + 3] * f + x.w * g;
+                }
+        }
+    }
+    if (wave || !valid) return;
+    write_rows<T, D>(a, it, state.o, m, l, col, sq.first + token, head, half);
+}
+
+// ------------------------------------------------------------------ chunks
+
+constexpr int CHUNK_ROWS = 128, CHUNK_KEYS = 64;
+
+// 128 rows against a range of keys, 32 rows a wave, in tiles of 64 keys that the
+// workgroup shares through LDS (two buffers: the next tile is loaded to
+// registers while this one is worked on, and written to the other buffer).
+// Bound by the matrix products and the exponentials between them.
+template <class T, bool F8, int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
+    constexpr int PER_ROW = F8 ? D / 16 : D / 8;            // 16-byte pieces of a cache entry
+    constexpr int PIECES = CHUNK_KEYS * PER_ROW / 256;      // of one thread
+    constexpr int TILE = CHUNK_KEYS * D * 2;
+    __shared__ __attribute__((aligned(16))) char lds[2][2][TILE];
+    __shared__ uint64_t odd_of[2][4];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+    const Item it = find_item(a, false, blockIdx.x);
+    if (!it.there) return;
+    const uint32_t tid = threadIdx.x, lane = tid & (WAVE - 1), half = lane / 32, wave = uniform(tid / WAVE), col = lane % 32;
+    const Seq &sq = it.shape.q;
+    const uint32_t rows = sq.rows * a.group, r0 = it.row_tile * CHUNK_ROWS, row = r0 + wave * 32 + col;
+    uint32_t flip;
+    bool zero;
+    const float c = score_factor(a, it.head, &flip, &zero);
+    const bool valid = row < rows;
+    const uint32_t token = a.by_group.div(valid ? row : 0), head = it.head * a.group + (valid ? row - token * a.group : 0);
+    int32_t first = 0, last = 0x7FFFFFFF;
+    if (valid) seen_by_row(a, sq, token, &first, &last);
+    int32_t all_first = first, all_last = last;   // keys that every row of the wave sees
+#pragma unroll
+    for (int step = 1; step < 32; step *= 2) {
+        all_first = max(all_first, __shfl_xor(all_first, step, WAVE));
+        all_last = min(all_last, __shfl_xor(all_last, step, WAVE));
+    }
+    all_first = (int32_t)uniform((uint32_t)all_first);
+    all_last = (int32_t)uniform((uint32_t)all_last);
+    // the tile's own keys, and those that all its rows see, inside the item's range
+    const uint32_t i0 = a.by_group.div(r0), i1 = a.by_group.div(min(r0 + CHUNK_ROWS, rows) - 1);
+    const Range own = seen(a, sq, i0, i1);
+    int32_t wg_first, wg_last, unused;
+    seen_by_row(a, sq, i1, &wg_first, &unused);
+    seen_by_row(a, sq, i0, &unused, &wg_last);
+    const uint32_t from = it.shape.keys.lo + it.split * it.length * CHUNK_KEYS;
+    const uint64_t past = (uint64_t)from + (uint64_t)it.length * CHUNK_KEYS;
+    const uint32_t k_lo = max(from, own.lo & ~(CHUNK_KEYS - 1u)), k_hi = (uint32_t)min((uint64_t)own.hi, past);
+    uint4 q[D / 16];
+    load_query<D>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
+    const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
+
+    uint4 k[PIECES], v[PIECES];
+    uint32_t entry[PIECES], off[PIECES];
+    auto look_up = [&](uint32_t k0) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t j = min(k0 + (tid + 256 * i) / PER_ROW, k_hi - 1), p = a.kv.by_page.div(j);
+            off[i] = j - p * a.kv.page;
+            entry[i] = table[p];
+        }
+    };
+    const uint32_t n_piece = tid % PER_ROW, o_piece = n_piece * 16 < a.kv.dim * (F8 ? 1 : 2) ? n_piece * 16 : 0;
+    const bool past_dim = n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
+    auto load = [&]() {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint64_t at = entry_at(a.kv, page_of(a.kv, entry[i]), off[i], it.head) + o_piece;
+            k[i] = *(const uint4 *)(a.kv.k + at);
+            v[i] = *(const uint4 *)(a.kv.v + at);
+        }
+    };
+    auto is_edge = [&](uint32_t k0) {
+        return (int32_t)k0 < wg_first || (int32_t)(k0 + CHUNK_KEYS - 1) > wg_last || k0 + CHUNK_KEYS > k_hi;
+    };
+    auto store = [&](int buf, bool edge) {
+        uint64_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t r = (tid + 256 * i) / PER_ROW;
+            if (past_dim) k[i] = make_uint4(0, 0, 0, 0);
+            uint4 x[2] = {k[i], k[i]}, y[2] = {v[i], v[i]};
+            if (F8) {
+                expand<T>(k[i], &x[0], &x[1]);
+                expand<T>(v[i], &y[0], &y[1]);
+            }
+#pragma unroll
+            for (int e = 0; e < (F8 ? 2 : 1); ++e) {
+                const uint32_t at = piece_at<D>(r, n_piece * (F8 ? 2 : 1) + e);
+                if (edge && drop_not_finite<T>(&y[e])) mine |= 1ull << r;
+                *(uint4 *)(lds[buf][0] + at) = x[e];
+                *(uint4 *)(lds[buf][1] + at) = y[e];
+            }
+        }
+        if (edge && ballot(mine != 0)) {
+#pragma unroll
+            for (int step = 1; step < WAVE; step *= 2) mine |= __shfl_xor((unsigned long long)mine, step, WAVE);
+        }
+        if (lane == 0) odd_of[buf][wave] = mine;
+    };
+    Rows<T, D> state;
+    state.clear();
+    if (k_lo < k_hi) {
+        look_up(k_lo);
+        load();
+        if (k_lo + CHUNK_KEYS < k_hi) look_up(k_lo + CHUNK_KEYS);
+        store(0, is_edge(k_lo));
+        __syncthreads();
+    }
+    int buf = 0;
+    for (uint32_t k0 = k_lo; k0 < k_hi; k0 += CHUNK_KEYS) {
+        const uint32_t next = k0 + CHUNK_KEYS;
+        if (next < k_hi) {
+            load();
+            if (next + CHUNK_KEYS < k_hi) look_up(next + CHUNK_KEYS);
+        }
+        const char *kt = lds[buf][0], *vt = lds[buf][1];
+        f32x16 s[2] = {f32x16(0.f), f32x16(0.f)};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                s[b] = T::mfma(*(const uint4 *)(kt + piece_at<D>(32 * b + col, dim_of_step(i, half) / 8)), q[i], s[b]);
+        if ((int32_t)k0 < all_first || (int32_t)(k0 + CHUNK_KEYS - 1) > all_last || next > k_hi) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int32_t key = (int32_t)(k0 + 32 * b + key_of(r, half));
+                    if (key < first || key > last || key >= (int32_t)k_hi) s[b][r] = MINUS_INF;
+                }
+        }
+        uint4 p[4];
+        state.template weigh<2>(s, c, p);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) state.add(vt, 16 * t, p[t]);
+        if (is_edge(k0)) {
+            const uint64_t odd = odd_of[buf][0] | odd_of[buf][1] | odd_of[buf][2] | odd_of[buf][3];
+            if (odd) add_not_finite<T, F8, D, 2>(state, s, odd, a, it.seq, it.head, k0, first, min(last, (int32_t)k_hi - 1));
+        }
+        if (next < k_hi) store(buf ^ 1, is_edge(next));
+        __syncthreads();
+        buf ^= 1;
+    }
+    if (!valid) return;
+    const float m = state.m == MINUS_INF ? MINUS_INF : state.m * c;
+    const float l = sum_of_halves(state.l);
+    write_rows<T, D>(a, it, state.o, m, l, row - r0, sq.first + token, head, half);
+}
+
+// -------------------------------------------------------------------- join
+
+constexpr uint32_t WEIGH_KEYS = 1024;   // keys of one (sequence, head) per workgroup
+
+// A row's maximum (base 2) and sum over its parts, by the lanes of a team of `team`
+// consecutive lanes (every lane gets them).
+__device__ __forceinline__ float2 join_stats(const AttnArgs &a, const Item &it, uint32_t head, uint32_t tile, uint32_t at,
+                                             uint32_t lane, uint32_t team) {
+    float m = MINUS_INF, l = 0.f;
+    for (uint32_t p = lane; p < it.splits; p += team) {
+        const uint32_t slot = slot_of(a, it, head, tile, p);
+        const float2 x = slot < a.slots ? a.part_ml[(uint64_t)slot * a.slot_rows + at] : make_float2(MINUS_INF, 0.f);
+        const float top = fmaxf(m, x.x), ref = top == MINUS_INF ? 0.f : top;
+        l = l * exp2_fast(m - ref) + x.y * exp2_fast(x.x - ref);
+        m = top;
+    }
+    for (uint32_t step = 1; step < team; step *= 2) {
+        const float m2 = __shfl_xor(m, step, WAVE), l2 = __shfl_xor(l, step, WAVE);
+        const float top = fmaxf(m, m2), ref = top == MINUS_INF ? 0.f : top;
+        l = l * exp2_fast(m - ref) + l2 * exp2_fast(m2 - ref);
+        m = top;
+    }
+    return make_float2(m, l);
+}
+
+// The parts of one token's rows, `teams` of D / 4 lanes to a row, each over every
+// teams-th part; and the whole call's status, for which the workgroups share the
+// table's entries.  Behind those workgroups, with few rows: the weights, from the scores.
+template <class T, int D>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t head_blocks, uint32_t key_blocks) {
+    constexpr uint32_t LANES = D / 4, ALL = 256 / LANES;
+    __shared__ float4 sums[256];
+    __shared__ float2 stats[32];
+    const uint32_t tid = threadIdx.x, joins = a.n_rows * head_blocks;
+    if (blockIdx.x < joins) {
+        // status
+        bool bad = false;
+        if (blockIdx.x == 0 && tid == 0) bad = a.q_off[0] != 0 || a.q_off[a.n_seqs] != a.n_rows;
+        const uint32_t share = joins > a.n_seqs ? joins / a.n_seqs : 1;   // workgroups to a sequence
+        for (uint32_t b = blockIdx.x; b < a.n_seqs * share; b += joins) {
+            const uint32_t s = b / share, part = b - s * share;
+            bool wrong;
+            const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &wrong);
+            bad |= wrong || q.rows > a.max_q || q.rows > q.len;
+            if (!q.rows) continue;
+            const Range r = seen(a, q, 0, q.rows - 1);
+            if (r.lo >= r.hi) continue;
+            const uint32_t p1 = a.kv.by_page.div(r.hi - 1);
+            for (uint32_t p = a.kv.by_page.div(r.lo) + part * 256 + tid; p <= p1; p += share * 256)
+                bad |= a.table[(uint64_t)s * a.table_stride + p] >= a.kv.n_pages;
+        }
+        if (bad) atomicOr(a.status, DEV_ERR_BAD_LAYOUT);
+        // join
+        const uint32_t t = blockIdx.x / head_blocks, rows = ALL / teams;
+        const uint32_t s = seq_of(a.q_off, a.n_seqs, t);
+        const Item it = find_item(a, true, s);
+        const Seq &q = it.shape.q;
+        if (!it.there || it.splits < 2 || t < q.first || t - q.first >= q.rows) return;
+        const uint32_t at = tid / LANES, lane = tid % LANES, team = at % teams;
+        const uint32_t e = (blockIdx.x - t * head_blocks) * rows + at / teams;
+        const bool there = e < a.n_heads;
+        const uint32_t ee = there ? e : 0;
+        const uint32_t h = a.by_group.div(ee), r = (t - q.first) * a.group + ee - h * a.group;
+        const uint32_t tile = r / a.row_tile, row = r - tile * a.row_tile;
+        const float2 ml = join_stats(a, it, h, tile, row, lane, LANES);
+        const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t p = team; p < it.splits; p += teams) {
+            const uint32_t slot = slot_of(a, it, h, tile, p);
+            if (slot >= a.slots) continue;
+            const uint64_t i = (uint64_t)slot * a.slot_rows + row;
+            const float m = a.part_ml[i].x;
+            if (m == MINUS_INF) continue;
+            const float4 x = *(const float4 *)(a.part + i * D + lane * 4);
+            const float f = exp2_fast(m - ref);
+            sum = make_float4(sum.x + x.x * f, sum.y + x.y * f, sum.z + x.z * f, sum.w + x.w * f);
+        }
+        sums[tid] = sum;
+        __syncthreads();
+        if (team || !there) return;
+        for (uint32_t i = 1; i < teams; ++i) {
+            const float4 x = sums[tid + i * LANES];
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+        }
+        const bool none = ml.x == MINUS_INF;
+        const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[h] : 1.f) / ml.y;
+        const float base2 = none ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+        if (lane == 0) {
+            if (a.lse) a.lse[(uint64_t)t * a.n_heads + e] = base2 * LN2;
+            if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + e] = base2;
+        }
+        if (lane * 4 < a.kv.dim)
+            *(uint2 *)(a.out + (uint64_t)t * a.o_row + e * a.o_head + lane * 8) =
+                make_uint2(T::pack(sum.x * f, sum.y * f), T::pack(sum.z * f, sum.w * f));
+        return;
+    }
+    // weights of WEIGH_KEYS keys of one (sequence, head) from the scores
+    const uint32_t b = blockIdx.x - joins, s = b / (key_blocks * a.kv.n_kv), hk = b - s * key_blocks * a.kv.n_kv;
+    const uint32_t h = hk / key_blocks, k0 = (hk - h * key_blocks) * WEIGH_KEYS;
+    const Item it = find_item(a, true, s);
+    const Seq &q = it.shape.q;
+    const uint32_t rows = q.rows * a.group;
+    const uint32_t r = tid / 8;   // 32 teams of 8
+    if (r < rows) {
+        float base2;
+        if (it.splits > 1) {
+            const float2 ml = join_stats(a, it, h, 0, r, tid % 8, 8);
+            base2 = ml.x == MINUS_INF ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+        } else {
+            const uint32_t i = a.by_group.div(r);
+            base2 = a.lse2[(uint64_t)(q.first + i) * a.n_heads + h * a.group + (r - i * a.group)];
+        }
+        // a row that sees nothing adds exp2(-inf - inf) = 0
+        if (tid % 8 == 0) stats[r].x = base2 == MINUS_INF ? __builtin_inff() : base2;
+    }
+    __syncthreads();
+    const uint64_t row = (uint64_t)s * a.kv.n_kv + h;
+    for (uint32_t j = k0 + tid; j < min(k0 + WEIGH_KEYS, a.max_kv); j += 256) {
+        float w = 0.f;
+        if (j < q.len) {
+            w = a.weight ? a.weight[row * a.weight_stride + j] : 0.f;
+            if (j >= it.shape.keys.lo && j < it.shape.keys.hi) {
+                const float *x = a.scores + row * a.slot_rows * a.score_stride + j;
+                float sum = 0.f;
+#pragma unroll 8
+                for (uint32_t i = 0; i < rows; ++i) sum += exp2_fast(x[i * a.score_stride] - stats[i].x);
+                w += sum;
+            }
+        }
+        a.weight_out[row * a.weight_stride + j] = w;
+    }
+}
+
+// ----------------------------------------------------------------- weights
+
+constexpr int WEIGHT_KEYS = 256, WEIGHT_ROWS = 64;
+
+// Of a chunk: 256 keys against all rows that see them (or one part of the
+// rows), 64 keys a wave in registers as the right operand of scores = Q K^T, the rows
+// passing through LDS.  With the statistics known there is no running maximum: a
+// register holds one row, so a key's sum is a sum over registers.  Bound by the
+// matrix products and exponentials, about half of the attention's.
+template <class T, bool F8, int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs a, uint32_t key_blocks) {
+    constexpr int PIECES = D / 8 * WEIGHT_ROWS / 256;
+    constexpr int TILE = WEIGHT_ROWS * D * 2;
+    __shared__ __attribute__((aligned(16))) char lds[2][TILE];
+    __shared__ __attribute__((aligned(16))) float base2[2][WEIGHT_ROWS];
+    __shared__ __attribute__((aligned(16))) int32_t slot_of_row[2][WEIGHT_ROWS];
+    const uint32_t tid = threadIdx.x, lane = tid & (WAVE - 1), half = lane / 32, wave = uniform(tid / WAVE), col = lane % 32;
+    uint32_t b = blockIdx.x;
+    const uint32_t h = b % a.kv.n_kv;
+    b /= a.kv.n_kv;
+    const uint32_t part = b % a.weight_parts;
+    b /= a.weight_parts;
+    const uint32_t s = b / key_blocks, k0 = (b - s * key_blocks) * WEIGHT_KEYS;
+    const Shape shape = shape_of(a, s);
+    const Seq &q = shape.q;
+    const uint64_t out_row = (uint64_t)s * a.kv.n_kv + h;
+    uint32_t flip;
+    bool zero;
+    const float c = score_factor(a, h, &flip, &zero);
+    float sum[2] = {0.f, 0.f};
+    const uint32_t k_lo = max(k0, shape.keys.lo), k_hi = min(min(k0 + WEIGHT_KEYS, shape.keys.hi), q.len);
+    if (k_lo < k_hi) {
+        // rows (token, head of the group) that see any of the keys, and this part of them
+        const int64_t j0 = (int64_t)q.len - q.rows;
+        int64_t i_lo = a.causal ? (int64_t)k_lo - j0 : 0, i_hi = a.window ? (int64_t)k_hi - 1 + a.window - j0 : q.rows;
+        i_lo = i_lo < 0 ? 0 : i_lo > (int64_t)q.rows ? (int64_t)q.rows : i_lo;
+        i_hi = i_hi < i_lo ? i_lo : i_hi > (int64_t)q.rows ? (int64_t)q.rows : i_hi;
+        const uint32_t r_all = (uint32_t)i_lo * a.group, r_past = (uint32_t)i_hi * a.group;
+        const uint32_t tiles = (r_past - r_all + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
+        const uint32_t each = (tiles + a.weight_parts - 1) / a.weight_parts;
+        const uint32_t r_lo = min(r_past, r_all + part * each * WEIGHT_ROWS), r_hi = min(r_past, r_lo + each * WEIGHT_ROWS);
+        // this lane's two keys
+        uint4 k[2][D / 16];
+        const uint32_t *table = a.table + (uint64_t)s * a.table_stride;
+        if (r_lo < r_hi) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const uint32_t j = min(k0 + wave * 64 + 32 * n + col, k_hi - 1), p = a.kv.by_page.div(j);
+                const char *base = a.kv.k + entry_at(a.kv, page_of(a.kv, table[p]), j - p * a.kv.page, h);
+#pragma unroll
+                for (int i = 0; i < D / 16; i += F8 ? 2 : 1) {
+                    const uint32_t d = dim_of_step(i, half), size = F8 ? 1 : 2;
+                    uint4 x = *(const uint4 *)(base + (d < a.kv.dim ? d * size : 0));
+                    if (d >= a.kv.dim) x = make_uint4(0, 0, 0, 0);
+                    if (F8) expand<T>(x, &k[n][i], &k[n][i + (F8 ? 1 : 0)]);
+                    else k[n][i] = x;
+                }
+            }
+        }
+        const uint32_t n_piece = tid % (D / 8);
+        uint4 x[PIECES];
+        float base = 0.f;
+        int32_t place = 0;
+        auto load = [&](uint32_t r0) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t r = r0 + (tid + 256 * i) / (D / 8);
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (r < r_hi && !zero && n_piece * 8 < a.kv.dim) {
+                    const uint32_t t = a.by_group.div(r), e = h * a.group + (r - t * a.group);
+                    const uint4 y = *(const uint4 *)(a.q + (uint64_t)(q.first + t) * a.q_row + e * a.q_head + n_piece * 16);
+                    x[i] = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
+                }
+            }
+            if (tid < WEIGHT_ROWS) {
+                base = __builtin_inff();   // exp2(-inf): rows past the end, rows that see nothing
+                place = 0;
+                if (r0 + tid < r_hi) {
+                    const uint32_t t = a.by_group.div(r0 + tid), e = h * a.group + (r0 + tid - t * a.group);
+                    const float y = a.lse2[(uint64_t)(q.first + t) * a.n_heads + e];
+                    base = y == MINUS_INF ? __builtin_inff() : y;
+                    place = (int32_t)(j0 + t);
+                }
+            }
+        };
+        auto store = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                *(uint4 *)(lds[buf] + piece_at<D>((tid + 256 * i) / (D / 8), n_piece)) = x[i];
+            if (tid < WEIGHT_ROWS) {
+                base2[buf][tid] = base;
+                slot_of_row[buf][tid] = place;
+            }
+        };
+        if (r_lo < r_hi) {
+            load(r_lo);
+            store(0);
+        }
+        __syncthreads();
+        int buf = 0;
+        const int32_t w_first = (int32_t)(k0 + wave * 64), w_last = w_first + 63;   // the wave's keys
+        for (uint32_t r0 = r_lo; r0 < r_hi; r0 += WEIGHT_ROWS) {
+            const bool more = r0 + WEIGHT_ROWS < r_hi;
+            if (more) load(r0 + WEIGHT_ROWS);
+            const int64_t x0 = j0 + a.by_group.div(r0), x1 = j0 + a.by_group.div(min(r0 + WEIGHT_ROWS, r_hi) - 1);
+            const bool edge = (a.causal && w_last > x0) || (a.window && (int64_t)w_first <= x1 - (int64_t)a.window) ||
+                              w_last >= (int32_t)k_hi;
+#pragma unroll
+            for (int m = 0; m < WEIGHT_ROWS / 32; ++m) {
+                f32x16 z[2] = {f32x16(0.f), f32x16(0.f)};
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint4 y = *(const uint4 *)(lds[buf] + piece_at<D>(32 * m + col, dim_of_step(i, half) / 8));
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) z[n] = T::mfma(y, k[n][i], z[n]);
+                }
+                float g[2] = {0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const float4 l = *(const float4 *)&base2[buf][32 * m + key_of(r, half)];
+                    const int4 place4 = *(const int4 *)&slot_of_row[buf][32 * m + key_of(r, half)];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        float e[4] = {exp2_fast(fmaf(z[n][r], c, -l.x)), exp2_fast(fmaf(z[n][r + 1], c, -l.y)),
+                                      exp2_fast(fmaf(z[n][r + 2], c, -l.z)), exp2_fast(fmaf(z[n][r + 3], c, -l.w))};
+                        if (edge) {
+                            const int32_t key = w_first + 32 * n + (int32_t)col;
+                            const int32_t at[4] = {place4.x, place4.y, place4.z, place4.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (key >= (int32_t)k_hi || (a.causal && key > at[i]) ||
+                                    (a.window && (int64_t)key <= (int64_t)at[i] - (int64_t)a.window))
+                                    e[i] = 0.f;
+                        }
+                        g[n] += (e[0] + e[1]) + (e[2] + e[3]);
+                    }
+                }
+                sum[0] += g[0];
+                sum[1] += g[1];
+            }
+            if (more) store(buf ^ 1);
+            __syncthreads();
+            buf ^= 1;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const float w = sum_of_halves(sum[n]);
+        const uint32_t j = k0 + wave * 64 + 32 * n + col;
+        if (half || j >= a.max_kv) continue;
+        if (a.weight_parts > 1) {
+            a.weight_part[((uint64_t)part * a.n_seqs * a.kv.n_kv + out_row) * a.max_kv + j] = w;
+        } else {
+            const float old = a.weight && j < q.len ? a.weight[out_row * a.weight_stride + j] : 0.f;
+            a.weight_out[out_row * a.weight_stride + j] = j < q.len ? old + w : 0.f;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void weight_sum_kernel(AttnArgs a, uint32_t key_blocks) {
+    const uint32_t row = blockIdx.x / key_blocks, s = row / a.kv.n_kv;
+    const uint32_t j = (blockIdx.x - row * key_blocks) * 256 + threadIdx.x;
+    if (j >= a.max_kv) return;
+    float w = 0.f;
+    if (j < a.kv_len[s]) {
+        w = a.weight ? a.weight[(uint64_t)row * a.weight_stride + j] : 0.f;
+        float sum = 0.f;
+        for (uint32_t p = 0; p < a.weight_parts; ++p)
+            sum += a.weight_part[((uint64_t)p * a.n_seqs * a.kv.n_kv + row) * a.max_kv + j];
+        w += sum;
+    }
+    a.weight_out[(uint64_t)row * a.weight_stride + j] = w;
+}
+
+// ---------------------------------------------------------------------- host
+
+constexpr uint32_t ROWS_MOST = 32;           // rows of the path for few rows
+constexpr uint32_t ROWS_ITEMS = 1024, CHUNK_ITEMS = 512;
+constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
+constexpr uint32_t WEIGHT_ITEMS = 1024;
+
+struct AttnPlan {
+    bool few;
+    uint32_t dim, slots, slot_rows, weight_parts, key_blocks;
+    uint64_t score_stride;
+};
+static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim) {
+    AttnPlan p;
+    const uint32_t group = n_heads / n_kv;
+    p.few = (uint64_t)max_q * group <= ROWS_MOST;
+    p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+    // an item that is a part has more than half an item's tiles: at most two per item wanted
+    p.slots = 2 * (p.few ? ROWS_ITEMS : CHUNK_ITEMS);
+    p.slot_rows = p.few ? (max_q ? max_q : 1) * group : CHUNK_ROWS;
+    p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
+    p.key_blocks = (uint32_t)(((uint64_t)max_kv + WEIGHT_KEYS - 1) / WEIGHT_KEYS);
+    const uint64_t blocks = (uint64_t)n_seqs * n_kv * (p.key_blocks ? p.key_blocks : 1);
+    const uint64_t tiles = ((uint64_t)max_q * group + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
+    uint64_t parts = blocks ? WEIGHT_ITEMS / blocks : 1;
+    parts = parts < tiles / 4 ? parts : tiles / 4;
+    p.weight_parts = (uint32_t)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+    return p;
+}
+static size_t attn_carve(AttnArgs *a, const AttnPlan &p, char *ws, uint32_t n_seqs, uint32_t n_rows, uint32_t max_kv,
+                         uint32_t n_heads, uint32_t n_kv, bool weights) {
+    Carver c{ws, 0};
+    a->status = c.take<int32_t>(WS_HEADER / 4);
+    a->part = c.take<float>((size_t)p.slots * p.slot_rows * p.dim);
+    a->part_ml = c.take<float2>((size_t)p.slots * p.slot_rows);
+    a->lse2 = nullptr;
+    a->scores = a->weight_part = nullptr;
+    if (weights) {
+        a->lse2 = c.take<float>((size_t)n_rows * n_heads);
+        if (p.few) a->scores = c.take<float>((size_t)n_seqs * n_kv * p.slot_rows * p.score_stride);
+        else if (p.weight_parts > 1) a->weight_part = c.take<float>((size_t)p.weight_parts * n_seqs * n_kv * max_kv);
+    }
+    a->slots = p.slots;
+    a->slot_rows = p.slot_rows;
+    a->score_stride = p.score_stride;
+    a->weight_parts = p.weight_parts;
+    return c.off;
+}
+
+template <class T, bool F8, int D>
+static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t items, hipStream_t st) {
+    if (p.few) {
+        if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, true>), dim3((unsigned)items), dim3(256), 0, st, a);
+        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, false>), dim3((unsigned)items), dim3(256), 0, st, a);
+    } else {
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D>), dim3((unsigned)items), dim3(256), 0, st, a);
+    }
+    // few joins take several teams to a row
+    constexpr uint32_t ALL = 256 / (D / 4);
+    uint32_t teams = ALL;
+    while (teams > 1 && (uint64_t)a.n_rows * a.n_heads * teams / ALL > 4096) teams /= 2;
+    const uint32_t head_blocks = (a.n_heads + ALL / teams - 1) / (ALL / teams);
+    const uint32_t key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
+    const uint64_t joins = (uint64_t)a.n_rows * head_blocks;
+    const uint64_t weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * key_blocks : 0;
+    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(joins + weigh)), dim3(256), 0, st, a, teams, head_blocks, key_blocks);
+    if (a.weight_out && !p.few && a.max_kv) {
+        const uint64_t blocks = (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks;
+        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D>), dim3((unsigned)(blocks * p.weight_parts)), dim3(256), 0, st, a, p.key_blocks);
+        if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, p.key_blocks);
+    }
+    return PC_OK;
+}
+template <class T, bool F8>
+static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, uint64_t items, hipStream_t st) {
+    if (p.dim == 64) return attn_run<T, F8, 64>(a, p, items, st);
+    if (p.dim == 128) return attn_run<T, F8, 128>(a, p, items, st);
+    return attn_run<T, F8, 256>(a, p, items, st);
+}
+
+}  // namespace pc
+
+extern "C" {
+
+size_t pc_attn_paged_ws(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32_t max_kv, uint32_t n_heads,
+                        uint32_t n_kv_heads, uint32_t head_dim, int with_weight) {
+    using namespace pc;
+    if (!n_heads || !n_kv_heads || n_heads % n_kv_heads) return WS_HEADER;
+    AttnArgs a;
+    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim);
+    return attn_carve(&a, p, nullptr, n_seqs, n_rows, max_kv, n_heads, n_kv_heads, with_weight != 0);
+}
+
+pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                        const uint32_t *kv_len, const uint32_t *q_off, uint32_t n_seqs, uint32_t n_rows,
+                        uint32_t max_q, uint32_t max_kv, const void *q, uint64_t q_stride_row,
+                        uint64_t q_stride_head, uint32_t dtype, uint32_t n_heads, float scale, uint32_t flags,
+                        uint32_t window, void *out, uint64_t out_stride_row, uint64_t out_stride_head, float *lse,
+                        const float *weight, float *weight_out, uint64_t weight_stride, void *ws, size_t ws_bytes,
+                        void *stream) {
+    using namespace pc;
+    AttnArgs a;
+    const pc_status ok = kv_view(cache, &a.kv);
+    if (ok != PC_OK) return ok;
+    if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
+    if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
+    if (!n_heads || n_heads > PC_MAX_HEADS || n_heads % a.kv.n_kv || flags & ~PC_ATTN_CAUSAL || !isfinite(scale))
+        return PC_ERR_INVALID;
+    if (max_kv > 0x7FFF0000u || (uint64_t)n_rows * n_heads > 0x7FFFFFFFu || (uint64_t)max_q * n_heads > 0x7FFFFFFFu)
+        return PC_ERR_TOO_LARGE;
+    if (max_kv > table_stride * a.kv.page || (weight_out && max_kv > weight_stride) || (weight && !weight_out))
+        return PC_ERR_INVALID;
+    if (n_rows && (!n_seqs || !max_q || !q || !out)) return PC_ERR_INVALID;
+    if (n_seqs && (!kv_len || !q_off || (max_kv && !page_table))) return PC_ERR_INVALID;
+    if (((uint64_t)(uintptr_t)q | (uint64_t)(uintptr_t)out | q_stride_row * 2 | q_stride_head * 2 | out_stride_row * 2 |
+         out_stride_head * 2) % 16)
+        return PC_ERR_INVALID;
+    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim);
+    const size_t need = attn_carve(&a, p, (char *)ws, n_seqs, n_rows, max_kv, n_heads, a.kv.n_kv, weight_out != nullptr);
+    if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
+    const hipStream_t st = (hipStream_t)stream;
+    a.table = page_table;
+    a.kv_len = kv_len;
+    a.q_off = q_off;
+    a.table_stride = table_stride;
+    a.n_seqs = n_seqs;
+    a.n_rows = n_rows;
+    a.max_q = max_q;
+    a.max_kv = max_kv;
+    a.q = (const char *)q;
+    a.out = (char *)out;
+    a.q_row = q_stride_row * 2;
+    a.q_head = q_stride_head * 2;
+    a.o_row = out_stride_row * 2;
+    a.o_head = out_stride_head * 2;
+    a.lse = lse;
+    a.weight = weight;
+    a.weight_out = weight_out;
+    a.weight_stride = weight_stride;
+    a.n_heads = n_heads;
+    a.group = n_heads / a.kv.n_kv;
+    a.by_group = fast_div(a.group);
+    a.scale = scale;
+    a.causal = flags & PC_ATTN_CAUSAL;
+    a.window = window;
+    a.target = p.few ? ROWS_ITEMS : CHUNK_ITEMS;
+    a.least = p.few ? ROWS_LEAST : CHUNK_LEAST;
+    a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;
+    a.key_tile = p.few ? 32 : CHUNK_KEYS;
+    if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
+    // as many items as there can be: the ones wanted, and one more for every tile of rows
+    const uint64_t tiles = p.few ? n_seqs : (uint64_t)n_rows * a.group / CHUNK_ROWS + n_seqs;
+    const uint64_t items = a.target + tiles * a.kv.n_kv;
+    if (items > 0x7FFFFFFFu || (uint64_t)n_seqs * a.kv.n_kv * ((uint64_t)p.key_blocks + 1) * 16 > 0x7FFFFFFFu)
+        return PC_ERR_TOO_LARGE;
+    const bool f8 = cache->dtype == PC_FP8_E4M3;
+    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, items, st) : attn_dim<Bf16, false>(a, p, items, st);
+    return f8 ? attn_dim<F16, true>(a, p, items, st) : attn_dim<F16, false>(a, p, items, st);
+}
+
+}  // extern "C"

@@ -76,6 +76,13 @@ enum KernelId {
     K_RUNS_FILL,
     K_BELADY_RANK,
     K_BELADY,
+    K_KV_APPEND,
+    K_KV_EVICT_SELECT,
+    K_KV_EVICT_MOVE,
+    K_ATTN_ROWS,
+    K_ATTN_CHUNK,
+    K_ATTN_JOIN,
+    K_ATTN_WEIGHT,
     K_MRC_MAP,
     K_COUNT
 };

@@ -1,0 +1,367 @@
+// The paged cache of KV blocks: new tokens written into it (pc_kv_append), and
+// sequences cut to the tokens with the most accumulated attention weight
+// (pc_kv_evict).
+#include "pc_kv.h"
+
+namespace pc {
+
+size_t type_size(uint32_t dtype) {
+    switch (dtype) {
+    case PC_BF16:
+    case PC_F16: return 2;
+    case PC_FP8_E4M3: return 1;
+    }
+    return 0;
+}
+
+pc_status kv_view(const pc_kv_cache *c, KvView *v) {
+    if (!c || !c->k || !c->v) return PC_ERR_INVALID;
+    const size_t size = type_size(c->dtype);
+    if (!size) return PC_ERR_INVALID;
+    const bool scaled = c->dtype == PC_FP8_E4M3;
+    if (scaled != (c->k_scale != nullptr) || scaled != (c->v_scale != nullptr)) return PC_ERR_INVALID;
+    if (c->page_size < 1 || c->page_size > PC_MAX_PAGE || c->n_kv_heads < 1 || c->n_kv_heads > PC_MAX_HEADS)
+        return PC_ERR_INVALID;
+    if (c->head_dim < 16 || c->head_dim > PC_MAX_HEAD_DIM || c->head_dim % 16 || c->n_pages < 1) return PC_ERR_INVALID;
+    if (c->n_pages == PC_NONE) return PC_ERR_TOO_LARGE;
+    // every access is of 16 bytes at a multiple of 16
+    const uint64_t bits = (uint64_t)(uintptr_t)c->k | (uint64_t)(uintptr_t)c->v | c->stride_page * size |
+                          c->stride_head * size | c->stride_slot * size;
+    if (bits % 16) return PC_ERR_INVALID;
+    *v = KvView{(char *)c->k, (char *)c->v, c->k_scale, c->v_scale, c->stride_page * size, c->stride_head * size,
+                c->stride_slot * size, c->n_pages, c->n_kv_heads, c->head_dim, c->page_size, fast_div(c->page_size)};
+    return PC_OK;
+}
+
+// ------------------------------------------------------------------- append
+// A copy with an index: bound by memory, or for a few tokens by the one launch
+// and its chain of loads (the row's sequence, its length, its page).
+
+struct AppendArgs {
+    KvView kv;
+    const uint32_t *table, *kv_len, *q_off;
+    uint64_t table_stride;
+    uint32_t n_seqs, n_rows, max_kv;
+    const char *k, *v;   // strides in bytes
+    uint64_t k_row, k_head, v_row, v_head;
+    int32_t *status;
+    FastDiv by_head;     // 16-byte pieces of one head's cache entry
+    uint32_t pieces;     // of one token
+};
+
+// One word for the whole call, by the first workgroup: it looks at every
+// sequence and every page that the call writes (a lane per page, 64 sequences at
+// a time), so that no launch is spent on clearing a word that the others would set.
+__device__ void append_status(const AppendArgs &a) {
+    __shared__ int32_t wrong;
+    if (threadIdx.x == 0) wrong = 0;
+    __syncthreads();
+    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE, waves = blockDim.x / WAVE;
+    bool any = threadIdx.x == 0 && (a.q_off[0] != 0 || a.q_off[a.n_seqs] != a.n_rows);
+    for (uint32_t s0 = wave * WAVE; s0 < a.n_seqs; s0 += waves * WAVE) {
+        const uint32_t s = s0 + lane;
+        uint32_t from = 0, pages = 0;
+        if (s < a.n_seqs) {
+            bool bad;
+            const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
+            any |= bad || q.rows > q.len;
+            if (q.rows && q.len) {
+                from = a.kv.by_page.div(q.rows < q.len ? q.len - q.rows : 0);
+                pages = a.kv.by_page.div(q.len - 1) + 1 - from;
+            }
+        }
+        const uint32_t end = wave_incl_scan(pages), all = (uint32_t)__shfl((int)end, WAVE - 1, WAVE);
+        for (uint32_t p0 = 0; p0 < all; p0 += WAVE) {
+            const uint32_t p = p0 + lane;
+            int at = 0;   // sequence of page p: the first lane whose end is past it
+#pragma unroll
+            for (int step = WAVE / 2; step; step /= 2)
+                if ((uint32_t)__shfl((int)end, at + step - 1, WAVE) <= p) at += step;
+            at = at < WAVE ? at : WAVE - 1;
+            const uint32_t e = (uint32_t)__shfl((int)end, at, WAVE), n = (uint32_t)__shfl((int)pages, at, WAVE),
+                           f = (uint32_t)__shfl((int)from, at, WAVE);
+            if (p < all) any |= a.table[(uint64_t)(s0 + at) * a.table_stride + f + (p - (e - n))] >= a.kv.n_pages;
+        }
+    }
+    if (any) wrong = DEV_ERR_BAD_LAYOUT;
+    __syncthreads();
+    if (threadIdx.x == 0) *a.status = wrong;
+}
+
+__device__ __forceinline__ float to_float(uint32_t bits, bool bf16) {
+    if (bf16) return __uint_as_float(bits << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+
+// four elements (two words) to four codes
+template <bool BF16>
+__device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b, float scale) {
+    float x[4] = {to_float(a & 0xFFFF, BF16), to_float(a >> 16, BF16), to_float(b & 0xFFFF, BF16), to_float(b >> 16, BF16)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float y = x[i] / scale;
+        x[i] = y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+    }
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
+    return (uint32_t)w;
+}
+
+// MODE 0: the types agree; 1, 2: an 8-bit cache from bf16, f16
+template <int MODE>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+    if (blockIdx.x == 0) {
+        append_status(a);
+        return;
+    }
+    // a wave per token
+    const int lane = threadIdx.x & (WAVE - 1);
+    const uint32_t t = (blockIdx.x - 1) * (256 / WAVE) + threadIdx.x / WAVE;
+    if (t >= a.n_rows) return;
+    const uint32_t s = seq_of(a.q_off, a.n_seqs, t);
+    bool bad;
+    const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
+    if (t < q.first || t - q.first >= q.rows) return;
+    const int64_t slot = (int64_t)q.len - q.rows + (t - q.first);
+    if (slot < 0) return;
+    const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;
+    const uint32_t page = a.table[(uint64_t)s * a.table_stride + at];
+    if (page >= a.kv.n_pages) return;
+    const uint64_t to = page * a.kv.sp + off * a.kv.st;
+    for (uint32_t p = lane; p < a.pieces; p += WAVE) {
+        const uint32_t h = a.by_head.div(p), c = p - h * a.by_head.d;
+        const uint64_t dst = to + h * a.kv.sh + c * 16;
+        const uint4 *k = (const uint4 *)(a.k + t * a.k_row + h * a.k_head) + c * (MODE ? 2 : 1);
+        const uint4 *v = (const uint4 *)(a.v + t * a.v_row + h * a.v_head) + c * (MODE ? 2 : 1);
+        if (MODE == 0) {
+            const uint4 x = *k, y = *v;
+            *(uint4 *)(a.kv.k + dst) = x;
+            *(uint4 *)(a.kv.v + dst) = y;
+        } else {
+            const uint4 x0 = k[0], x1 = k[1], y0 = v[0], y1 = v[1];
+            const float ks = a.kv.k_scale[h], vs = a.kv.v_scale[h];
+            *(uint4 *)(a.kv.k + dst) = make_uint4(to_e4m3<MODE == 1>(x0.x, x0.y, ks), to_e4m3<MODE == 1>(x0.z, x0.w, ks),
+                                                  to_e4m3<MODE == 1>(x1.x, x1.y, ks), to_e4m3<MODE == 1>(x1.z, x1.w, ks));
+            *(uint4 *)(a.kv.v + dst) = make_uint4(to_e4m3<MODE == 1>(y0.x, y0.y, vs), to_e4m3<MODE == 1>(y0.z, y0.w, vs),
+                                                  to_e4m3<MODE == 1>(y1.x, y1.y, vs), to_e4m3<MODE == 1>(y1.z, y1.w, vs));
+        }
+    }
+}
+
+// -------------------------------------------------------------------- evict
+
+struct EvictArgs {
+    KvView kv;
+    const uint32_t *table, *kv_len, *dst_table;
+    uint64_t table_stride, dst_stride, weight_stride;
+    uint32_t n_seqs, max_kv, budget, recent;
+    const float *weight;
+    uint32_t *kept, *new_len;
+    float *weight_out;
+    int32_t *status;
+    FastDiv by_piece;   // 16-byte pieces of one entry
+};
+
+// floats as integers of the same order; the zeros are one value, and so are the NaN, above all others
+__device__ __forceinline__ uint32_t order_of(float f) {
+    if (f != f) return 0xFFFFFFFFu;
+    const uint32_t b = __float_as_uint(f + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+constexpr int SELECT_THREADS = 1024;
+
+// One workgroup per (sequence, head): the need-th largest key by four digits of
+// eight bits (a histogram each), then the kept slots in order.
+__global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs a) {
+    __shared__ uint32_t hist[256], tmp[2 * SELECT_THREADS / WAVE];
+    __shared__ uint32_t pick, left;
+    const uint32_t s = blockIdx.x / a.kv.n_kv, h = blockIdx.x - s * a.kv.n_kv, tid = threadIdx.x;
+    if (blockIdx.x == 0) {   // the call's status word; the pages are the move's to check
+        bool bad = false;
+        for (uint32_t i = tid; i < a.n_seqs; i += SELECT_THREADS) bad |= a.kv_len[i] > a.max_kv;
+        const int any = __syncthreads_or(bad);
+        if (tid == 0) *a.status = any ? DEV_ERR_BAD_LAYOUT : 0;
+    }
+    const uint32_t len = min(a.kv_len[s], a.max_kv), n = min(len, a.budget), late = min(a.recent, n);
+    const uint32_t cand = len - late, need = n - late;   // need of the first cand slots stay
+    const uint64_t row = (uint64_t)s * a.kv.n_kv + h;
+    const float *w = a.weight + row * a.weight_stride;
+    uint32_t *kept = a.kept + row * a.budget;
+    float *wout = a.weight_out ? a.weight_out + row * a.budget : nullptr;
+    if (h == 0 && tid == 0) a.new_len[s] = n;
+    uint32_t floor_key = 0, equal = need;   // keys above floor_key stay, and `equal` of those at it
+    if (need < cand && need > 0) {
+        uint32_t known = 0, mask = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256) hist[tid] = 0;
+            __syncthreads();
+            for (uint32_t j = tid; j < cand; j += SELECT_THREADS) {
+                const uint32_t key = order_of(w[j]);
+                if ((key & mask) == known) atomicAdd(&hist[key >> shift & 255], 1u);
+            }
+            __syncthreads();
+            uint32_t total;
+            const uint32_t c = tid < 256 ? hist[255 - tid] : 0;
+            const uint32_t above = block_excl_scan(c, tmp, &total);   // digits larger than 255 - tid
+            if (tid < 256 && above < equal && above + c >= equal) {
+                pick = 255 - tid;
+                left = equal - above;
+            }
+            __syncthreads();
+            known |= pick << shift;
+            mask |= 255u << shift;
+            equal = left;
+            __syncthreads();
+        }
+        floor_key = known;
+    }
+    const bool all = need == cand;
+    uint32_t placed = 0, ties = 0;
+    for (uint32_t j0 = 0; j0 < len; j0 += SELECT_THREADS) {
+        const uint32_t j = j0 + tid;
+        const float x = j < len ? w[j] : 0.f;
+        const uint32_t key = order_of(x);
+        const bool in = j < cand && need > 0;
+        const bool tie = in && !all && key == floor_key;
+        uint32_t t_all, k_all;
+        const uint32_t t = ties + block_excl_scan(tie, tmp, &t_all);
+        const bool keep = (j >= cand && j < len) || (in && (all || key > floor_key || (tie && t < equal)));
+        const uint32_t at = placed + block_excl_scan(keep, tmp, &k_all);
+        if (keep) {
+            kept[at] = j;
+            if (wout) wout[at] = x;
+        }
+        ties += t_all;
+        placed += k_all;
+    }
+    for (uint32_t r = n + tid; r < a.budget; r += SELECT_THREADS) {
+        kept[r] = NONE;
+        if (wout) wout[r] = 0.f;
+    }
+}
+
+constexpr uint32_t MOVE_SLOTS = 64;   // slots of one (sequence, head) per workgroup
+
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t groups) {
+    const uint32_t row = blockIdx.x / groups, r0 = (blockIdx.x - row * groups) * MOVE_SLOTS;
+    const uint32_t s = row / a.kv.n_kv, h = row - s * a.kv.n_kv;
+    const uint32_t n = min(min(a.kv_len[s], a.max_kv), a.budget);
+    if (r0 >= n) return;
+    const uint32_t slots = min(MOVE_SLOTS, n - r0), pieces = slots * a.by_piece.d;
+    for (uint32_t p = threadIdx.x; p < pieces; p += 256) {
+        const uint32_t i = a.by_piece.div(p), c = p - i * a.by_piece.d, r = r0 + i;
+        const uint32_t j = a.kept[(uint64_t)row * a.budget + r];
+        const uint32_t js = a.kv.by_page.div(j), rs = a.kv.by_page.div(r);
+        const uint32_t from = a.table[(uint64_t)s * a.table_stride + js], to = a.dst_table[(uint64_t)s * a.dst_stride + rs];
+        if (from >= a.kv.n_pages || to >= a.kv.n_pages) {
+            atomicOr(a.status, DEV_ERR_BAD_LAYOUT);
+            continue;
+        }
+        const uint64_t src = from * a.kv.sp + h * a.kv.sh + (j - js * a.kv.page) * a.kv.st + c * 16;
+        const uint64_t dst = to * a.kv.sp + h * a.kv.sh + (r - rs * a.kv.page) * a.kv.st + c * 16;
+        const uint4 x = *(const uint4 *)(a.kv.k + src), y = *(const uint4 *)(a.kv.v + src);
+        *(uint4 *)(a.kv.k + dst) = x;
+        *(uint4 *)(a.kv.v + dst) = y;
+    }
+}
+
+}  // namespace pc
+
+extern "C" {
+
+size_t pc_kv_append_ws(void) { return pc::WS_HEADER; }
+
+pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                       const uint32_t *kv_len, const uint32_t *q_off, uint32_t n_seqs, uint32_t n_rows,
+                       uint32_t max_kv, const void *k, uint64_t k_stride_row, uint64_t k_stride_head,
+                       const void *v, uint64_t v_stride_row, uint64_t v_stride_head, uint32_t dtype, void *ws,
+                       size_t ws_bytes, void *stream) {
+    using namespace pc;
+    AppendArgs a;
+    const pc_status ok = kv_view(cache, &a.kv);
+    if (ok != PC_OK) return ok;
+    if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
+    if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
+    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u) return PC_ERR_TOO_LARGE;
+    if (max_kv > table_stride * a.kv.page) return PC_ERR_INVALID;
+    if (!kv_len || !q_off || (max_kv && !page_table) || (n_rows && (!k || !v))) return PC_ERR_INVALID;
+    if (((uint64_t)(uintptr_t)k | (uint64_t)(uintptr_t)v | k_stride_row * 2 | k_stride_head * 2 | v_stride_row * 2 |
+         v_stride_head * 2) % 16)
+        return PC_ERR_INVALID;
+    if (n_seqs == 0 && n_rows) return PC_ERR_INVALID;
+    if (!ws || ws_bytes < pc_kv_append_ws()) return PC_ERR_WORKSPACE;
+    const hipStream_t st = (hipStream_t)stream;
+    a.table = page_table;
+    a.kv_len = kv_len;
+    a.q_off = q_off;
+    a.table_stride = table_stride;
+    a.n_seqs = n_seqs;
+    a.n_rows = n_rows;
+    a.max_kv = max_kv;
+    a.k = (const char *)k;
+    a.v = (const char *)v;
+    a.k_row = k_stride_row * 2;
+    a.k_head = k_stride_head * 2;
+    a.v_row = v_stride_row * 2;
+    a.v_head = v_stride_head * 2;
+    a.status = (int32_t *)ws;
+    a.by_head = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
+    a.pieces = a.by_head.d * a.kv.n_kv;
+    const unsigned grid = 1 + (n_rows + 3) / 4;
+    if (cache->dtype != PC_FP8_E4M3) PC_LAUNCH(K_KV_APPEND, append_kernel<0>, dim3(grid), dim3(256), 0, st, a);
+    else if (dtype == PC_BF16) PC_LAUNCH(K_KV_APPEND, append_kernel<1>, dim3(grid), dim3(256), 0, st, a);
+    else PC_LAUNCH(K_KV_APPEND, append_kernel<2>, dim3(grid), dim3(256), 0, st, a);
+    return PC_OK;
+}
+
+size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv) {
+    (void)n_seqs;
+    (void)n_kv_heads;
+    (void)max_kv;
+    return pc::WS_HEADER;
+}
+
+pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                      const uint32_t *kv_len, uint32_t n_seqs, uint32_t max_kv, const float *weight,
+                      uint64_t weight_stride, uint32_t budget, uint32_t recent, const uint32_t *dst_table,
+                      uint64_t dst_stride, uint32_t *kept, float *weight_out, uint32_t *new_len, void *ws,
+                      size_t ws_bytes, void *stream) {
+    using namespace pc;
+    EvictArgs a;
+    const pc_status ok = kv_view(cache, &a.kv);
+    if (ok != PC_OK) return ok;
+    if (budget < 1 || recent > budget) return PC_ERR_INVALID;
+    if (max_kv > 0x7FFF0000u || budget > 0x7FFF0000u || (uint64_t)n_seqs * a.kv.n_kv > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
+    if (max_kv > weight_stride) return PC_ERR_INVALID;
+    if (n_seqs && (!kv_len || !kept || !new_len || (max_kv && !weight))) return PC_ERR_INVALID;
+    if (dst_table && (max_kv > table_stride * a.kv.page || budget > dst_stride * a.kv.page || (max_kv && !page_table)))
+        return PC_ERR_INVALID;
+    if (!ws || ws_bytes < pc_kv_evict_ws(n_seqs, a.kv.n_kv, max_kv)) return PC_ERR_WORKSPACE;
+    const hipStream_t st = (hipStream_t)stream;
+    if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
+    a.table = page_table;
+    a.kv_len = kv_len;
+    a.dst_table = dst_table;
+    a.table_stride = table_stride;
+    a.dst_stride = dst_stride;
+    a.weight_stride = weight_stride;
+    a.n_seqs = n_seqs;
+    a.max_kv = max_kv;
+    a.budget = budget;
+    a.recent = recent;
+    a.weight = weight;
+    a.kept = kept;
+    a.new_len = new_len;
+    a.weight_out = weight_out;
+    a.status = (int32_t *)ws;
+    a.by_piece = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
+    const unsigned rows = n_seqs * a.kv.n_kv;
+    const uint32_t groups = (budget < max_kv ? budget : max_kv) / MOVE_SLOTS + 1;
+    if (dst_table && (uint64_t)rows * groups > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
+    PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
+    if (dst_table) PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel, dim3(rows * groups), dim3(256), 0, st, a, groups);
+    return PC_OK;
+}
+
+}  // extern "C"

@@ -37,6 +37,13 @@ class PcError(RuntimeError):
     pass
 
 
+class _KvCache(ctypes.Structure):
+    """pc_kv_cache"""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("stride_page", _u64),
+                ("stride_head", _u64), ("stride_slot", _u64), ("dtype", _u32), ("n_pages", _u32), ("page_size", _u32),
+                ("n_kv_heads", _u32), ("head_dim", _u32)]
+
+
 def lib():
     """Load libpc.so (raises if it has not been built)."""
     global _lib
@@ -109,6 +116,21 @@ def lib():
     L.pc_belady_ws.argtypes = [_u64, _u32]
     L.pc_belady.restype = _st
     L.pc_belady.argtypes = [_vp, _vp, _u64, _vp, _u32, _vp, _vp, _vp, _vp, _sz, _vp]
+    L.pc_kv_append_ws.restype = _sz
+    L.pc_kv_append_ws.argtypes = []
+    L.pc_kv_append.restype = _st
+    L.pc_kv_append.argtypes = [_vp, _vp, _u64, _vp, _vp, _u32, _u32, _u32, _vp, _u64, _u64, _vp, _u64, _u64, _u32,
+                               _vp, _sz, _vp]
+    L.pc_attn_paged_ws.restype = _sz
+    L.pc_attn_paged_ws.argtypes = [_u32, _u32, _u32, _u32, _u32, _u32, _u32, ctypes.c_int]
+    L.pc_attn_paged.restype = _st
+    L.pc_attn_paged.argtypes = [_vp, _vp, _u64, _vp, _vp, _u32, _u32, _u32, _u32, _vp, _u64, _u64, _u32, _u32,
+                                ctypes.c_float, _u32, _u32, _vp, _u64, _u64, _vp, _vp, _vp, _u64, _vp, _sz, _vp]
+    L.pc_kv_evict_ws.restype = _sz
+    L.pc_kv_evict_ws.argtypes = [_u32, _u32, _u32]
+    L.pc_kv_evict.restype = _st
+    L.pc_kv_evict.argtypes = [_vp, _vp, _u64, _vp, _u32, _u32, _vp, _u64, _u32, _u32, _vp, _u64, _vp, _vp, _vp, _vp,
+                              _sz, _vp]
     L.pc_workspace_status.restype = _st
     L.pc_workspace_status.argtypes = [_vp, _sz, _vp, ctypes.POINTER(ctypes.c_int32)]
     L.pc_prof_enable.restype = None
@@ -483,6 +505,179 @@ def belady(nxt: torch.Tensor, caps: torch.Tensor, depth: Optional[torch.Tensor] 
     check(L.pc_belady(_ptr(nxt), _ptr(depth), n, _ptr(caps), k, _ptr(out["hits"]), _ptr(out["depthsum"]),
                       _ptr(out.get("flags")) if flags else None, _ptr(ws), ws.numel(), _stream()))
     return out, ws
+
+
+# ------------------------------------------------------------- paged cache
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}   # PC_BF16, PC_F16, PC_FP8_E4M3
+
+
+def _table(t: torch.Tensor, what: str, rows: int):
+    """A table of 32-bit integers or floats, [rows, columns] with the columns contiguous: (address, row stride)."""
+    if not t.is_cuda:
+        raise PcError("expected a GPU tensor")
+    if t.element_size() != 4 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise PcError("%s: expected [%d, columns] of 32 bits, columns contiguous" % (what, rows))
+    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1]
+
+
+def _index(t: torch.Tensor, what: str):
+    if t.element_size() != 4 or t.is_floating_point() or t.dim() != 1:
+        raise PcError("%s: expected one dimension of 32-bit integers" % what)
+    return _ptr(t)
+
+
+def _rows(t: torch.Tensor, what: str, heads: int, dim: int):
+    """New tokens [rows, heads, head_dim], head_dim contiguous: (address, row stride, head stride)."""
+    if not t.is_cuda:
+        raise PcError("expected a GPU tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1:
+        raise PcError("%s: expected [rows, %d, %d], the last dimension contiguous" % (what, heads, dim))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else dim, t.stride(1) if heads > 1 else dim
+
+
+class PagedCache:
+    """A paged cache of KV blocks (``pc_kv_cache``) over two tensors [page, head,
+    slot, head_dim] of one type and one set of strides, head_dim contiguous: pages
+    kept as [page, slot, head, head_dim] go in as ``x.transpose(1, 2)``.  bfloat16,
+    float16, or float8_e4m3fn with ``k_scale`` and ``v_scale`` (float32, one per head)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
+            raise PcError("expected two tensors [page, head, slot, head_dim] of bfloat16, float16 or float8_e4m3fn")
+        if not (k.is_cuda and v.is_cuda):
+            raise PcError("expected a GPU tensor")
+        if k.stride(3) != 1 or any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1):
+            raise PcError("expected equal strides of k and v, head_dim contiguous")
+        for x in (k_scale, v_scale):
+            if x is not None and (x.dtype != torch.float32 or x.numel() != k.shape[1]):
+                raise PcError("expected one float32 scale per head")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        size = [s if n > 1 else self.head_dim for s, n in zip(k.stride(), k.shape)]
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), size[0], size[1], size[2],
+                           _DTYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
+
+    def _ref(self):
+        return ctypes.addressof(self._c)
+
+
+def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, q_off: torch.Tensor,
+              k: torch.Tensor, v: torch.Tensor, max_kv: Optional[int] = None, ws: Optional[torch.Tensor] = None):
+    """pc_kv_append: rows q_off[s] .. q_off[s + 1] - 1 of ``k`` and ``v`` ([rows, head,
+    head_dim]) into the last slots of the kv_len[s] of sequence s."""
+    L = lib()
+    n_seqs = kv_len.numel()
+    table, stride = _table(page_table, "page_table", n_seqs)
+    if max_kv is None:
+        max_kv = min(page_table.shape[1] * cache.page_size, 0x7FFF0000)
+    if k.dtype != v.dtype or k.dtype not in _DTYPES or k.shape != v.shape or q_off.numel() != n_seqs + 1:
+        raise PcError("expected k and v of one shape and type, and one offset more than sequences")
+    if max_kv > page_table.shape[1] * cache.page_size:
+        raise PcError("max_kv: the page table has fewer slots")
+    ka, kr, kh = _rows(k, "k", cache.n_kv_heads, cache.head_dim)
+    va, vr, vh = _rows(v, "v", cache.n_kv_heads, cache.head_dim)
+    if ws is None:
+        ws = workspace(L.pc_kv_append_ws())
+    check(L.pc_kv_append(cache._ref(), table, stride, _index(kv_len, "kv_len"), _index(q_off, "q_off"), n_seqs,
+                         k.shape[0], max_kv, ka, kr, kh, va, vr, vh, _DTYPES[k.dtype], _ptr(ws), ws.numel(), _stream()))
+    return ws
+
+
+def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor,
+               q_off: torch.Tensor, max_q: int, max_kv: Optional[int] = None, scale: Optional[float] = None,
+               causal: bool = True, window: int = 0, out: Optional[torch.Tensor] = None, want_lse: bool = False,
+               lse: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+               weight_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """pc_attn_paged: attention of the new tokens ``q`` [rows, query head, head_dim]
+    over the cache, which holds their keys and values already.  ``max_q`` and
+    ``max_kv`` bound a sequence's new rows and its length (max_kv: the page table's
+    room if not given); ``scale`` is 1 / sqrt(head_dim) if not given.  Returns
+    (out, lse or None, weight_out or None, ws); the accumulated weights
+    ([sequence, kv head, max_kv] float32) are formed when ``weight`` or ``weight_out``
+    is given."""
+    L = lib()
+    n_seqs = kv_len.numel()
+    table, stride = _table(page_table, "page_table", n_seqs)
+    if q.dim() != 3 or q.dtype not in _DTYPES or q_off.numel() != n_seqs + 1:
+        raise PcError("expected q as [rows, heads, head_dim], and one offset more than sequences")
+    n_rows, n_heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise PcError("q: the cache's head_dim is %d" % cache.head_dim)
+    if max_kv is None:
+        max_kv = min(page_table.shape[1] * cache.page_size, 0x7FFF0000)
+    if max_kv > page_table.shape[1] * cache.page_size:
+        raise PcError("max_kv: the page table has fewer slots")
+    if out is None:
+        out = torch.empty((n_rows, n_heads, dim), dtype=q.dtype, device=q.device)
+    if out.dtype != q.dtype or out.shape[0] != n_rows:
+        raise PcError("out: expected q's type and rows")
+    if lse is None and want_lse:
+        lse = torch.empty((n_rows, n_heads), dtype=torch.float32, device=q.device)
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n_rows, n_heads)):
+        raise PcError("lse: expected [rows, heads] float32")
+    if weight_out is None and weight is not None:
+        weight_out = torch.empty((n_seqs, cache.n_kv_heads, max_kv), dtype=torch.float32, device=q.device)
+    strides = set()
+    for name, w in (("weight", weight), ("weight_out", weight_out)):
+        if w is None:
+            continue
+        if w.dtype != torch.float32 or tuple(w.shape[:2]) != (n_seqs, cache.n_kv_heads) or w.dim() != 3 or \
+                w.shape[2] < max_kv:
+            raise PcError("%s: expected [sequences, kv heads, at least max_kv] float32" % name)
+        _ptr(w)
+        strides.add(w.shape[2])
+    if len(strides) > 1:
+        raise PcError("weight and weight_out: expected one shape")
+    qa, qr, qh = _rows(q, "q", n_heads, dim)
+    oa, o_r, oh = _rows(out, "out", n_heads, dim)
+    if ws is None:
+        ws = workspace(L.pc_attn_paged_ws(n_seqs, n_rows, max_q, max_kv, n_heads, cache.n_kv_heads, dim,
+                                          1 if weight_out is not None else 0))
+    check(L.pc_attn_paged(cache._ref(), table, stride, _index(kv_len, "kv_len"), _index(q_off, "q_off"), n_seqs, n_rows,
+                          max_q, max_kv, qa, qr, qh, _DTYPES[q.dtype], n_heads, dim ** -0.5 if scale is None else scale,
+                          1 if causal else 0, window, oa, o_r, oh, _ptr(lse), _ptr(weight), _ptr(weight_out),
+                          strides.pop() if strides else 0, _ptr(ws), ws.numel(), _stream()))
+    return out, lse, weight_out, ws
+
+
+def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, weight: torch.Tensor, budget: int,
+             recent: int, dst_table: Optional[torch.Tensor] = None, max_kv: Optional[int] = None,
+             out: Optional[dict] = None, ws: Optional[torch.Tensor] = None):
+    """pc_kv_evict: per (sequence, head) the last ``recent`` slots and those of the
+    largest ``weight`` ([sequence, kv head, max_kv] float32), ``budget`` in all, in slot order.
+    Their keys and values move to the pages of ``dst_table`` when it is given.  Returns
+    {"kept" (int32, -1 behind the last), "weight", "new_len", "ws"}."""
+    L = lib()
+    n_seqs = kv_len.numel()
+    table, stride = _table(page_table, "page_table", n_seqs)
+    if weight.dtype != torch.float32 or weight.dim() != 3 or tuple(weight.shape[:2]) != (n_seqs, cache.n_kv_heads):
+        raise PcError("weight: expected [sequences, kv heads, slots] float32")
+    if max_kv is None:
+        max_kv = min(page_table.shape[1] * cache.page_size, weight.shape[2])
+    if max_kv > page_table.shape[1] * cache.page_size or max_kv > weight.shape[2]:
+        raise PcError("max_kv: the page table or the weights have fewer slots")
+    dst, dst_stride = (None, 0) if dst_table is None else _table(dst_table, "dst_table", n_seqs)
+    if dst_table is not None and dst_table.shape[1] * cache.page_size < budget:
+        raise PcError("dst_table: room for fewer than budget slots")
+    shape = (n_seqs, cache.n_kv_heads, budget)
+    if out is None:
+        out = {"kept": torch.empty(shape, dtype=torch.int32, device=weight.device),
+               "weight": torch.empty(shape, dtype=torch.float32, device=weight.device),
+               "new_len": torch.empty(n_seqs, dtype=torch.int32, device=weight.device)}
+    for name in ("kept", "weight"):
+        if out.get(name) is not None and (tuple(out[name].shape) != shape or out[name].element_size() != 4):
+            raise PcError("%s: expected [sequences, kv heads, budget] of 32 bits" % name)
+    if out["new_len"].numel() != n_seqs or out["new_len"].element_size() != 4:
+        raise PcError("new_len: expected one 32-bit integer per sequence")
+    if ws is None:
+        ws = workspace(L.pc_kv_evict_ws(n_seqs, cache.n_kv_heads, max_kv))
+    check(L.pc_kv_evict(cache._ref(), table, stride, _index(kv_len, "kv_len"), n_seqs, max_kv, _ptr(weight),
+                        weight.shape[2], budget, recent, dst, dst_stride, _ptr(out["kept"]), _ptr(out.get("weight")),
+                        _ptr(out["new_len"]), _ptr(ws), ws.numel(), _stream()))
+    out["ws"] = ws
+    return out
 
 
 def bins_to_host(out: dict) -> dict:

@@ -192,8 +192,10 @@ struct Item {
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
-// by_seq: the sequence `key` as a whole (slot: its first); else item number `key`
-__device__ __forceinline__ Item find_item(const AttnArgs &a, bool by_seq, uint32_t key) {
+// What `key` counts: items; tiles of rows of every head (whatever their ranges); sequences.
+enum class By { ITEM, TILE, SEQ };
+template <By BY>
+__device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
     const int lane = threadIdx.x & (WAVE - 1);
     Item it;
     it.there = false;
@@ -212,23 +214,22 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, bool by_seq, uint32
     uint64_t base = 0, slot = 0;
     for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
         const uint32_t s = s0 + lane;
-        uint32_t items = 0, splits = 1;
+        uint32_t items = 0, splits = 1, count = 0;
         if (s < a.n_seqs) {
             if (a.n_seqs > WAVE) h = shape_of(a, s);
             splits = (h.key_tiles + it.length - 1) / it.length;
             splits = splits ? splits : 1;
             const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
             items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
+            count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
         }
-        const uint32_t end = wave_incl_scan(items), partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
+        const uint32_t partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
+        const uint32_t end = BY == By::SEQ ? 0 : wave_incl_scan(count);
         int at;
-        if (by_seq) {
-            at = key >= s0 && key - s0 < WAVE ? (int)(key - s0) : WAVE;
-        } else {
-            at = __popcll(ballot(base + end <= key));
-        }
+        if (BY == By::SEQ) at = key - s0 < WAVE ? (int)(key - s0) : WAVE;
+        else at = __popcll(ballot(base + end <= key));
         at = (int)uniform((uint32_t)at);
-        if (at < WAVE) {
+        if (at < WAVE && s0 + at < a.n_seqs) {
             it.there = true;
             it.seq = s0 + at;
             it.splits = from_lane(splits, at);
@@ -241,16 +242,16 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, bool by_seq, uint32
             it.shape.key_tiles = from_lane(h.key_tiles, at);
             it.slot = (uint32_t)slot + from_lane(slot_end - partial, at);
             it.head = it.row_tile = it.split = 0;
-            if (!by_seq) {
+            if (BY != By::SEQ) {
                 // heads first (neighbouring workgroups are on different XCDs, so with 2, 4 or 8
                 // heads an L2 holds one or few heads' keys), then rows, the last ones first
                 // (they see the most keys), then ranges
-                const uint32_t i = key - (uint32_t)(base + from_lane(end - items, at));
-                it.slot += i;
-                it.head = i % a.kv.n_kv;
+                const uint32_t i = key - (uint32_t)(base + from_lane(end - count, at));
                 const uint32_t j = i / a.kv.n_kv;
-                it.row_tile = it.shape.row_tiles - 1 - j % it.shape.row_tiles;
+                it.head = i - j * a.kv.n_kv;
                 it.split = j / it.shape.row_tiles;
+                it.row_tile = it.shape.row_tiles - 1 - (j - it.split * it.shape.row_tiles);
+                if (BY == By::ITEM) it.slot += i;
             }
             return it;
         }
@@ -259,7 +260,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, bool by_seq, uint32
     }
     return it;
 }
-// slot of an item of a sequence found by_seq
+// slot of an item, from the sequence's first (found by tile or by sequence)
 __device__ __forceinline__ uint32_t slot_of(const AttnArgs &a, const Item &it, uint32_t head, uint32_t row_tile, uint32_t split) {
     return it.slot + (split * it.shape.row_tiles + (it.shape.row_tiles - 1 - row_tile)) * a.kv.n_kv + head;
 }
@@ -272,14 +273,14 @@ __device__ __forceinline__ uint32_t slot_of(const AttnArgs &a, const Item &it, u
 constexpr __device__ __forceinline__ uint32_t dim_of_step(uint32_t step, uint32_t half) {
     return 32 * (step / 2) + 16 * half + 8 * (step % 2);
 }
-template <int D>
+template <int D, bool FULL>
 __device__ __forceinline__ void load_query(const AttnArgs &a, const char *row, bool there, uint32_t half, uint32_t flip,
                                            bool zero, uint4 (&q)[D / 16]) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
         const uint32_t d = dim_of_step(s, half);
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (there && !zero && d < a.kv.dim) {
+        if (there && !zero && (FULL || d < a.kv.dim)) {
             x = *(const uint4 *)(row + d * 2);
             x = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
         }

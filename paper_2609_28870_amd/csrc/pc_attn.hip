@@ -34,48 +34,39 @@ __device__ __forceinline__ bool drop_not_finite(uint4 *x) {
     return any;
 }
 
-// Values that are not finite, where rows differ in which keys they see: the
-// matrix product would carry 0 * inf = NaN to rows that do not see the key.  There the
-// tile was written without them, and they are added here to the rows that do.
-// Rare, so it is written for size: one key at a time.
-template <class T, bool F8, int D, int B>
-__device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const f32x16 (&p)[B], uint64_t keys, const AttnArgs &a,
-                                               uint32_t seq, uint32_t head, uint32_t k0, int32_t first, int32_t last) {
-    const uint32_t half = threadIdx.x / 32 % 2;
-    while (keys) {
-        const uint32_t i = (uint32_t)__builtin_ctzll(keys), key = k0 + i, in = i % 32, reg = in / 8 * 4 + in % 4;
-        keys &= keys - 1;
-        float mine = 0.f;
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (b == (int)(i / 32) && r == (int)reg) mine = p[b][r];
-        float lower, upper;
-        both_halves(mine, &lower, &upper);
-        const float w = in / 4 % 2 ? upper : lower;
-        const bool visible = (int32_t)key >= first && (int32_t)key <= last;
-        const uint32_t at = a.kv.by_page.div(key);
-        const uint32_t page = page_of(a.kv, a.table[(uint64_t)seq * a.table_stride + at]);
-        const char *v = a.kv.v + entry_at(a.kv, page, key - at * a.kv.page, head);
+// Values that are not finite, in tiles whose keys some rows see and some do not: the
+// matrix product would carry 0 * inf = NaN to rows that do not see the key.  Such a
+// tile is worked on without them, and where there were any they are added here, after
+// the loop, to the rows that see them: key by key, the scores formed again.  Rare,
+// so written for size.  `query` is this lane's row of 16-bit elements.
+template <class T, bool F8, int D, class Query>
+__device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs &a, uint32_t seq, uint32_t head, uint32_t key,
+                                               int32_t first, int32_t last, float c, Query query) {
+    const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32;
+    const uint32_t at = a.kv.by_page.div(key), page = page_of(a.kv, a.table[(uint64_t)seq * a.table_stride + at]);
+    const uint64_t entry = entry_at(a.kv, page, key - at * a.kv.page, head);
+    auto element = [&](const char *base, uint32_t d) {
+        if (F8) return T::value(T::template from_e4m3<false>(*(const uint8_t *)(base + entry + d)) & 0xFFFF);
+        return T::value(*(const uint16_t *)(base + entry + 2 * d));
+    };
+    bool odd = false;
+    for (uint32_t d = lane; d < a.kv.dim; d += WAVE) odd |= !(fabsf(element(a.kv.v, d)) < __builtin_inff());
+    if (!ballot(odd)) return;
+    float s = 0.f;
 #pragma unroll 1
-        for (int b = 0; b < D / 32; ++b) {
-            f32x16 add = f32x16(0.f);
+    for (uint32_t d = half; d < a.kv.dim; d += 2) s = fmaf(T::value(query(d)), element(a.kv.k, d), s);
+    s = sum_of_halves(s);
+    const float p = exp2_fast(fmaf(s, c, T::TOP - state.m * c));
+    const bool visible = (int32_t)key >= first && (int32_t)key <= last;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t d = 32 * b + key_of(r, half);
-                if (d < a.kv.dim) {
-                    float x;
-                    if (F8) x = T::value(T::template from_e4m3<false>(*(const uint8_t *)(v + d)) & 0xFFFF);
-                    else x = T::value(*(const uint16_t *)(v + 2 * d));
-                    if (visible && !(fabsf(x) < __builtin_inff())) add[r] = w * x;
-                }
-            }
+    for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-            for (int bb = 0; bb < D / 32; ++bb)
-                if (bb == b) state.o[bb] += add;
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t d = 32 * b + key_of(r, half);
+            const float x = element(a.kv.v, d < a.kv.dim ? d : 0);
+            state.o[b][r] += visible && !(fabsf(x) < __builtin_inff()) ? p * x : 0.f;
+            if (r % 4 == 3) __asm__ volatile("" ::: "memory");   // few of the loads at once: the registers are full
         }
-    }
 }
 
 // A row's result: whole (its sequence is one item long), or a part for the join.
@@ -119,13 +110,15 @@ __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, co
 // item), the next tile's bytes on their way to its registers meanwhile.  Keys
 // go straight into the matrix product, a lane per key; values pass through
 // LDS for the transposed read.  The four waves' results are joined in LDS.
-template <class T, bool F8, int D, bool WEIGHTS>
+// FULL: the head has D dimensions, and no piece of a key is past them.
+template <class T, bool F8, int D, bool FULL, bool WEIGHTS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a) {
     constexpr int PIECES = F8 ? D / 32 : D / 16;   // 16 bytes, of one lane's half of a key
     __shared__ __attribute__((aligned(16))) char tiles[4 * 32 * D * 2];
+    __shared__ __attribute__((aligned(16))) char queries[32 * D * 2];   // the same for all waves
     __shared__ float2 join_ml[2][64];
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-    const Item it = find_item(a, false, blockIdx.x);
+    const Item it = find_item<By::ITEM>(a, blockIdx.x);
     if (!it.there) return;
     const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32, wave = uniform(threadIdx.x / WAVE), col = lane % 32;
     const Seq &sq = it.shape.q;
@@ -146,9 +139,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
     }
     all_first = (int32_t)uniform((uint32_t)all_first);
     all_last = (int32_t)uniform((uint32_t)all_last);
-    uint4 q[D / 16];
-    load_query<D>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
-
     const uint32_t t_end = min(it.shape.key_tiles, (it.split + 1) * it.length);
     uint32_t t = it.split * it.length + wave;
     const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
@@ -163,27 +153,46 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         off = j - p * a.kv.page;
         entry = table[p];
     };
-    auto piece = [&](int i) {   // its offset in the entry; past the head's dimensions, the first one
-        const uint32_t o = F8 ? 32 * i + 16 * half : 2 * dim_of_step(i, half);
-        return o < a.kv.dim * (F8 ? 1 : 2) ? o : 0;
-    };
     auto load = [&](const char *base, uint4 (&x)[PIECES]) {
+        const char *p = base + at + half * (F8 ? 16 : 32);
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) x[i] = *(const uint4 *)(base + at + piece(i));
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t o = F8 ? 32 * i : 2 * dim_of_step(i, 0);
+            // past the head's dimensions: its first ones
+            if (FULL || o + half * (F8 ? 16 : 32) < a.kv.dim * (F8 ? 1 : 2)) x[i] = *(const uint4 *)(p + o);
+            else x[i] = *(const uint4 *)(base + at);
+        }
     };
+    if (t < t_end) look_up(t);
+    uint4 q[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+        const uint32_t r = (threadIdx.x + 256 * i) / (D / 8), d = threadIdx.x % (D / 8) * 8, n = a.by_group.div(r);
+        q[i] = make_uint4(0, 0, 0, 0);
+        if (r < rows && !zero && (FULL || d < a.kv.dim)) {
+            const uint4 x = *(const uint4 *)(a.q + (uint64_t)(sq.first + n) * a.q_row +
+                                             (it.head * a.group + (r - n * a.group)) * a.q_head + d * 2);
+            q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+        }
+    }
     if (t < t_end) {
-        look_up(t);
         at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
         load(a.kv.k, k);
         load(a.kv.v, v);
         if (t + 4 < t_end) look_up(t + 4);
     }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+        *(uint4 *)(queries + piece_at<D>((threadIdx.x + 256 * i) / (D / 8), threadIdx.x % (D / 8))) = q[i];
+    __syncthreads();
+    bool odd = false;   // a value that is not finite was left out of a tile
+    auto query = [&](int i) { return *(const uint4 *)(queries + piece_at<D>(col, dim_of_step(i, half) / 8)); };
     for (; t < t_end; t += 4) {
         const bool more = t + 4 < t_end;
         const uint32_t k0 = it.shape.keys.lo + t * 32;
         const bool full = (int32_t)k0 >= all_first && (int32_t)k0 + 31 <= all_last;
         f32x16 s[1] = {f32x16(0.f)};
-        if (a.kv.dim != D) {
+        if (!FULL) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
                 if ((F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
@@ -193,16 +202,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
             if (F8) {
                 uint4 x, y;
                 expand<T>(k[i / 2], &x, &y);
-                s[0] = T::mfma(i % 2 ? y : x, q[i], s[0]);
+                s[0] = T::mfma(i % 2 ? y : x, query(i), s[0]);
             } else {
-                s[0] = T::mfma(k[i % PIECES], q[i], s[0]);
+                s[0] = T::mfma(k[i % PIECES], query(i), s[0]);
             }
         }
         if (more) {
             at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
             load(a.kv.k, k);
         }
-        uint64_t odd = 0;   // keys with values that are not finite, where rows differ
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t n = F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
@@ -210,10 +218,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
             if (F8) expand<T>(v[i], &x[0], &x[1]);
 #pragma unroll
             for (int e = 0; e < (F8 ? 2 : 1); ++e) {
-                if (!full) {
-                    const uint64_t b = ballot(drop_not_finite<T>(&x[e]));
-                    odd |= (b | b >> 32) & 0xFFFFFFFFull;
-                }
+                if (!full) odd |= drop_not_finite<T>(&x[e]);
                 *(uint4 *)(tile + piece_at<D>(col, n + e)) = x[e];
             }
         }
@@ -241,7 +246,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         state.add(tile, 0, p[0]);
         state.add(tile, 16, p[1]);
         __builtin_amdgcn_wave_barrier();
-        if (odd) add_not_finite<T, F8, D, 1>(state, s, odd, a, it.seq, it.head, k0, first, last);
+    }
+    if (ballot(odd)) {
+        for (t = it.split * it.length + wave; t < t_end; t += 4) {
+            const uint32_t k0 = it.shape.keys.lo + t * 32;
+            if ((int32_t)k0 >= all_first && (int32_t)k0 + 31 <= all_last) continue;
+            for (uint32_t key = k0; key < min(k0 + 32, it.shape.keys.hi); ++key)
+                add_not_finite<T, F8, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
+                    return *(const uint16_t *)(queries + piece_at<D>(col, d / 8) + d % 8 * 2);
+                });
+        }
     }
     float m = state.m == MINUS_INF ? MINUS_INF : state.m * c, l = sum_of_halves(state.l);
     // waves 2 and 3 to 0 and 1, then 1 to 0
@@ -282,21 +296,24 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
 
 // ------------------------------------------------------------------ chunks
 
-constexpr int CHUNK_ROWS = 128, CHUNK_KEYS = 64;
+constexpr int CHUNK_ROWS = 128;
+// keys of a tile: with 256 dimensions half as many, so that the registers hold out
+constexpr __host__ __device__ int chunk_keys(int d) { return d <= 128 ? 64 : 32; }
 
 // 128 rows against a range of keys, 32 rows a wave, in tiles of 64 keys that the
 // workgroup shares through LDS (two buffers: the next tile is loaded to
 // registers while this one is worked on, and written to the other buffer).
 // Bound by the matrix products and the exponentials between them.
-template <class T, bool F8, int D>
+template <class T, bool F8, int D, bool FULL>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
+    constexpr int CHUNK_KEYS = chunk_keys(D), BLOCKS = CHUNK_KEYS / 32;
     constexpr int PER_ROW = F8 ? D / 16 : D / 8;            // 16-byte pieces of a cache entry
     constexpr int PIECES = CHUNK_KEYS * PER_ROW / 256;      // of one thread
     constexpr int TILE = CHUNK_KEYS * D * 2;
     __shared__ __attribute__((aligned(16))) char lds[2][2][TILE];
-    __shared__ uint64_t odd_of[2][4];
+    __shared__ uint32_t odd;   // a value that is not finite was left out of a tile
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-    const Item it = find_item(a, false, blockIdx.x);
+    const Item it = find_item<By::ITEM>(a, blockIdx.x);
     if (!it.there) return;
     const uint32_t tid = threadIdx.x, lane = tid & (WAVE - 1), half = lane / 32, wave = uniform(tid / WAVE), col = lane % 32;
     const Seq &sq = it.shape.q;
@@ -326,7 +343,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     const uint64_t past = (uint64_t)from + (uint64_t)it.length * CHUNK_KEYS;
     const uint32_t k_lo = max(from, own.lo & ~(CHUNK_KEYS - 1u)), k_hi = (uint32_t)min((uint64_t)own.hi, past);
     uint4 q[D / 16];
-    load_query<D>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
+    load_query<D, FULL>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
     const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
 
     uint4 k[PIECES], v[PIECES];
@@ -339,8 +356,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
             entry[i] = table[p];
         }
     };
-    const uint32_t n_piece = tid % PER_ROW, o_piece = n_piece * 16 < a.kv.dim * (F8 ? 1 : 2) ? n_piece * 16 : 0;
-    const bool past_dim = n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
+    const uint32_t n_piece = tid % PER_ROW;
+    const bool past_dim = !FULL && n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
+    const uint32_t o_piece = past_dim ? 0 : n_piece * 16;
     auto load = [&]() {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -352,8 +370,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     auto is_edge = [&](uint32_t k0) {
         return (int32_t)k0 < wg_first || (int32_t)(k0 + CHUNK_KEYS - 1) > wg_last || k0 + CHUNK_KEYS > k_hi;
     };
+    if (tid == 0) odd = 0;
+    __syncthreads();
     auto store = [&](int buf, bool edge) {
-        uint64_t mine = 0;
+        bool mine = false;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t r = (tid + 256 * i) / PER_ROW;
@@ -366,16 +386,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
 #pragma unroll
             for (int e = 0; e < (F8 ? 2 : 1); ++e) {
                 const uint32_t at = piece_at<D>(r, n_piece * (F8 ? 2 : 1) + e);
-                if (edge && drop_not_finite<T>(&y[e])) mine |= 1ull << r;
+                if (edge) mine |= drop_not_finite<T>(&y[e]);
                 *(uint4 *)(lds[buf][0] + at) = x[e];
                 *(uint4 *)(lds[buf][1] + at) = y[e];
             }
         }
-        if (edge && ballot(mine != 0)) {
-#pragma unroll
-            for (int step = 1; step < WAVE; step *= 2) mine |= __shfl_xor((unsigned long long)mine, step, WAVE);
-        }
-        if (lane == 0) odd_of[buf][wave] = mine;
+        if (mine) odd = 1;
     };
     Rows<T, D> state;
     state.clear();
@@ -394,32 +410,40 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
             if (next + CHUNK_KEYS < k_hi) look_up(next + CHUNK_KEYS);
         }
         const char *kt = lds[buf][0], *vt = lds[buf][1];
-        f32x16 s[2] = {f32x16(0.f), f32x16(0.f)};
+        f32x16 s[BLOCKS];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < BLOCKS; ++b) s[b] = f32x16(0.f);
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
                 s[b] = T::mfma(*(const uint4 *)(kt + piece_at<D>(32 * b + col, dim_of_step(i, half) / 8)), q[i], s[b]);
         if ((int32_t)k0 < all_first || (int32_t)(k0 + CHUNK_KEYS - 1) > all_last || next > k_hi) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int32_t key = (int32_t)(k0 + 32 * b + key_of(r, half));
                     if (key < first || key > last || key >= (int32_t)k_hi) s[b][r] = MINUS_INF;
                 }
         }
-        uint4 p[4];
-        state.template weigh<2>(s, c, p);
+        uint4 p[2 * BLOCKS];
+        state.template weigh<BLOCKS>(s, c, p);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) state.add(vt, 16 * t, p[t]);
-        if (is_edge(k0)) {
-            const uint64_t odd = odd_of[buf][0] | odd_of[buf][1] | odd_of[buf][2] | odd_of[buf][3];
-            if (odd) add_not_finite<T, F8, D, 2>(state, s, odd, a, it.seq, it.head, k0, first, min(last, (int32_t)k_hi - 1));
-        }
+        for (int t = 0; t < 2 * BLOCKS; ++t) state.add(vt, 16 * t, p[t]);
         if (next < k_hi) store(buf ^ 1, is_edge(next));
         __syncthreads();
         buf ^= 1;
+    }
+    if (odd) {
+        const char *row_q = a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head;
+        for (uint32_t k0 = k_lo; k0 < k_hi; k0 += CHUNK_KEYS) {
+            if (!is_edge(k0)) continue;
+            for (uint32_t key = k0; key < min(k0 + CHUNK_KEYS, k_hi); ++key)
+                add_not_finite<T, F8, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
+                    return zero ? 0u : *(const uint16_t *)(row_q + 2 * d) ^ (flip & 0x8000u);
+                });
+        }
     }
     if (!valid) return;
     const float m = state.m == MINUS_INF ? MINUS_INF : state.m * c;
@@ -452,15 +476,16 @@ __device__ __forceinline__ float2 join_stats(const AttnArgs &a, const Item &it, 
     return make_float2(m, l);
 }
 
-// The parts of one token's rows, `teams` of D / 4 lanes to a row, each over every
+// The parts of some rows of a tile, `teams` of D / 4 lanes to a row, each over every
 // teams-th part; and the whole call's status, for which the workgroups share the
 // table's entries.  Behind those workgroups, with few rows: the weights, from the scores.
 template <class T, int D>
-__global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t head_blocks, uint32_t key_blocks) {
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t joins, uint32_t row_blocks,
+                                                   uint32_t key_blocks) {
     constexpr uint32_t LANES = D / 4, ALL = 256 / LANES;
     __shared__ float4 sums[256];
     __shared__ float2 stats[32];
-    const uint32_t tid = threadIdx.x, joins = a.n_rows * head_blocks;
+    const uint32_t tid = threadIdx.x;
     if (blockIdx.x < joins) {
         // status
         bool bad = false;
@@ -480,40 +505,41 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
         }
         if (bad) atomicOr(a.status, DEV_ERR_BAD_LAYOUT);
         // join
-        const uint32_t t = blockIdx.x / head_blocks, rows = ALL / teams;
-        const uint32_t s = seq_of(a.q_off, a.n_seqs, t);
-        const Item it = find_item(a, true, s);
-        const Seq &q = it.shape.q;
-        if (!it.there || it.splits < 2 || t < q.first || t - q.first >= q.rows) return;
+        const uint32_t tile = blockIdx.x / row_blocks;
+        const Item it = find_item<By::TILE>(a, tile);
+        if (!it.there || it.splits < 2) return;
         const uint32_t at = tid / LANES, lane = tid % LANES, team = at % teams;
-        const uint32_t e = (blockIdx.x - t * head_blocks) * rows + at / teams;
-        const bool there = e < a.n_heads;
-        const uint32_t ee = there ? e : 0;
-        const uint32_t h = a.by_group.div(ee), r = (t - q.first) * a.group + ee - h * a.group;
-        const uint32_t tile = r / a.row_tile, row = r - tile * a.row_tile;
-        const float2 ml = join_stats(a, it, h, tile, row, lane, LANES);
+        const uint32_t row = (blockIdx.x - tile * row_blocks) * (ALL / teams) + at / teams;   // of the tile
+        const uint32_t r = it.row_tile * a.row_tile + row;
+        const bool there = row < a.row_tile && r < it.shape.q.rows * a.group;
+        if ((blockIdx.x - tile * row_blocks) * (ALL / teams) + it.row_tile * a.row_tile >= it.shape.q.rows * a.group) return;
+        const uint32_t rr = there ? row : 0;
+        const float2 ml = join_stats(a, it, it.head, it.row_tile, rr, lane, LANES);
         const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (uint32_t p = team; p < it.splits; p += teams) {
-            const uint32_t slot = slot_of(a, it, h, tile, p);
+            const uint32_t slot = slot_of(a, it, it.head, it.row_tile, p);
             if (slot >= a.slots) continue;
-            const uint64_t i = (uint64_t)slot * a.slot_rows + row;
+            const uint64_t i = (uint64_t)slot * a.slot_rows + rr;
             const float m = a.part_ml[i].x;
             if (m == MINUS_INF) continue;
             const float4 x = *(const float4 *)(a.part + i * D + lane * 4);
             const float f = exp2_fast(m - ref);
             sum = make_float4(sum.x + x.x * f, sum.y + x.y * f, sum.z + x.z * f, sum.w + x.w * f);
         }
-        sums[tid] = sum;
-        __syncthreads();
+        if (teams > 1) {
+            sums[tid] = sum;
+            __syncthreads();
+        }
         if (team || !there) return;
         for (uint32_t i = 1; i < teams; ++i) {
             const float4 x = sums[tid + i * LANES];
             sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
         }
         const bool none = ml.x == MINUS_INF;
-        const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[h] : 1.f) / ml.y;
+        const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / ml.y;
         const float base2 = none ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+        const uint32_t i = a.by_group.div(r), t = it.shape.q.first + i, e = it.head * a.group + (r - i * a.group);
         if (lane == 0) {
             if (a.lse) a.lse[(uint64_t)t * a.n_heads + e] = base2 * LN2;
             if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + e] = base2;
@@ -526,7 +552,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
     // weights of WEIGH_KEYS keys of one (sequence, head) from the scores
     const uint32_t b = blockIdx.x - joins, s = b / (key_blocks * a.kv.n_kv), hk = b - s * key_blocks * a.kv.n_kv;
     const uint32_t h = hk / key_blocks, k0 = (hk - h * key_blocks) * WEIGH_KEYS;
-    const Item it = find_item(a, true, s);
+    const Item it = find_item<By::SEQ>(a, s);
     const Seq &q = it.shape.q;
     const uint32_t rows = q.rows * a.group;
     const uint32_t r = tid / 8;   // 32 teams of 8
@@ -569,7 +595,7 @@ constexpr int WEIGHT_KEYS = 256, WEIGHT_ROWS = 64;
 // passing through LDS.  With the statistics known there is no running maximum: a
 // register holds one row, so a key's sum is a sum over registers.  Bound by the
 // matrix products and exponentials, about half of the attention's.
-template <class T, bool F8, int D>
+template <class T, bool F8, int D, bool FULL>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs a, uint32_t key_blocks) {
     constexpr int PIECES = D / 8 * WEIGHT_ROWS / 256;
     constexpr int TILE = WEIGHT_ROWS * D * 2;
@@ -612,8 +638,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
 #pragma unroll
                 for (int i = 0; i < D / 16; i += F8 ? 2 : 1) {
                     const uint32_t d = dim_of_step(i, half), size = F8 ? 1 : 2;
-                    uint4 x = *(const uint4 *)(base + (d < a.kv.dim ? d * size : 0));
-                    if (d >= a.kv.dim) x = make_uint4(0, 0, 0, 0);
+                    const bool in = FULL || d < a.kv.dim;
+                    uint4 x = *(const uint4 *)(base + (in ? d * size : 0));
+                    if (!in) x = make_uint4(0, 0, 0, 0);
                     if (F8) expand<T>(x, &k[n][i], &k[n][i + (F8 ? 1 : 0)]);
                     else k[n][i] = x;
                 }
@@ -628,7 +655,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
             for (int i = 0; i < PIECES; ++i) {
                 const uint32_t r = r0 + (tid + 256 * i) / (D / 8);
                 x[i] = make_uint4(0, 0, 0, 0);
-                if (r < r_hi && !zero && n_piece * 8 < a.kv.dim) {
+                if (r < r_hi && !zero && (FULL || n_piece * 8 < a.kv.dim)) {
                     const uint32_t t = a.by_group.div(r), e = h * a.group + (r - t * a.group);
                     const uint4 y = *(const uint4 *)(a.q + (uint64_t)(q.first + t) * a.q_row + e * a.q_head + n_piece * 16);
                     x[i] = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
@@ -783,35 +810,40 @@ static size_t attn_carve(AttnArgs *a, const AttnPlan &p, char *ws, uint32_t n_se
     return c.off;
 }
 
-template <class T, bool F8, int D>
-static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t items, hipStream_t st) {
+template <class T, bool F8, int D, bool FULL>
+static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, hipStream_t st) {
+    // as many items as there can be: the ones wanted, and one more for every tile of rows
+    const dim3 items((unsigned)(a.target + tiles));
     if (p.few) {
-        if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, true>), dim3((unsigned)items), dim3(256), 0, st, a);
-        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, false>), dim3((unsigned)items), dim3(256), 0, st, a);
+        if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
+        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, false>), items, dim3(256), 0, st, a);
     } else {
-        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D>), dim3((unsigned)items), dim3(256), 0, st, a);
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL>), items, dim3(256), 0, st, a);
     }
     // few joins take several teams to a row
     constexpr uint32_t ALL = 256 / (D / 4);
     uint32_t teams = ALL;
-    while (teams > 1 && (uint64_t)a.n_rows * a.n_heads * teams / ALL > 4096) teams /= 2;
-    const uint32_t head_blocks = (a.n_heads + ALL / teams - 1) / (ALL / teams);
+    while (teams > 1 && tiles * p.slot_rows * teams / ALL > 4096) teams /= 2;
+    const uint32_t row_blocks = (p.slot_rows * teams + ALL - 1) / ALL;
     const uint32_t key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
-    const uint64_t joins = (uint64_t)a.n_rows * head_blocks;
+    const uint64_t joins = tiles * row_blocks;
     const uint64_t weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * key_blocks : 0;
-    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(joins + weigh)), dim3(256), 0, st, a, teams, head_blocks, key_blocks);
+    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(joins + weigh)), dim3(256), 0, st, a, teams, (uint32_t)joins,
+              row_blocks, key_blocks);
     if (a.weight_out && !p.few && a.max_kv) {
         const uint64_t blocks = (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks;
-        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D>), dim3((unsigned)(blocks * p.weight_parts)), dim3(256), 0, st, a, p.key_blocks);
+        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D, FULL>), dim3((unsigned)(blocks * p.weight_parts)), dim3(256), 0, st, a,
+                  p.key_blocks);
         if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, p.key_blocks);
     }
     return PC_OK;
 }
 template <class T, bool F8>
-static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, uint64_t items, hipStream_t st) {
-    if (p.dim == 64) return attn_run<T, F8, 64>(a, p, items, st);
-    if (p.dim == 128) return attn_run<T, F8, 128>(a, p, items, st);
-    return attn_run<T, F8, 256>(a, p, items, st);
+static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, hipStream_t st) {
+    const bool full = a.kv.dim == p.dim;
+    if (p.dim == 64) return full ? attn_run<T, F8, 64, true>(a, p, tiles, st) : attn_run<T, F8, 64, false>(a, p, tiles, st);
+    if (p.dim == 128) return full ? attn_run<T, F8, 128, true>(a, p, tiles, st) : attn_run<T, F8, 128, false>(a, p, tiles, st);
+    return full ? attn_run<T, F8, 256, true>(a, p, tiles, st) : attn_run<T, F8, 256, false>(a, p, tiles, st);
 }
 
 }  // namespace pc
@@ -880,18 +912,17 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.causal = flags & PC_ATTN_CAUSAL;
     a.window = window;
     a.target = p.few ? ROWS_ITEMS : CHUNK_ITEMS;
-    a.least = p.few ? ROWS_LEAST : CHUNK_LEAST;
+    a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;
-    a.key_tile = p.few ? 32 : CHUNK_KEYS;
+    a.key_tile = p.few ? 32 : chunk_keys(p.dim);
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
-    // as many items as there can be: the ones wanted, and one more for every tile of rows
-    const uint64_t tiles = p.few ? n_seqs : (uint64_t)n_rows * a.group / CHUNK_ROWS + n_seqs;
-    const uint64_t items = a.target + tiles * a.kv.n_kv;
-    if (items > 0x7FFFFFFFu || (uint64_t)n_seqs * a.kv.n_kv * ((uint64_t)p.key_blocks + 1) * 16 > 0x7FFFFFFFu)
+    // tiles of rows of every head, at most
+    const uint64_t tiles = (p.few ? n_seqs : (uint64_t)n_rows * a.group / CHUNK_ROWS + n_seqs) * (uint64_t)a.kv.n_kv;
+    if (tiles * p.slot_rows + a.target > 0x7FFFFFFFu || (uint64_t)n_seqs * a.kv.n_kv * ((uint64_t)p.key_blocks + 1) * 16 > 0x7FFFFFFFu)
         return PC_ERR_TOO_LARGE;
     const bool f8 = cache->dtype == PC_FP8_E4M3;
-    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, items, st) : attn_dim<Bf16, false>(a, p, items, st);
-    return f8 ? attn_dim<F16, true>(a, p, items, st) : attn_dim<F16, false>(a, p, items, st);
+    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, tiles, st) : attn_dim<Bf16, false>(a, p, tiles, st);
+    return f8 ? attn_dim<F16, true>(a, p, tiles, st) : attn_dim<F16, false>(a, p, tiles, st);
 }
 
 }  // extern "C"

@@ -510,30 +510,52 @@ def belady(nxt: torch.Tensor, caps: torch.Tensor, depth: Optional[torch.Tensor] 
 # ------------------------------------------------------------- paged cache
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}   # PC_BF16, PC_F16, PC_FP8_E4M3
+_MAX_KV = 0x7FFF0000
+
+
+def _stream_of(t: torch.Tensor):
+    """The current stream of a tensor's device, without the objects around it (a few
+    microseconds, as much as a small call's kernels take)."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _scratch(nbytes: int, t: torch.Tensor) -> torch.Tensor:
+    return torch.empty(nbytes, dtype=torch.uint8, device=t.device)
 
 
 def _table(t: torch.Tensor, what: str, rows: int):
-    """A table of 32-bit integers or floats, [rows, columns] with the columns contiguous: (address, row stride)."""
+    """A table of 32-bit integers, [rows, columns] with the columns contiguous: (address, row stride)."""
     if not t.is_cuda:
         raise PcError("expected a GPU tensor")
-    if t.element_size() != 4 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if t.element_size() != 4 or len(shape) != 2 or shape[0] != rows or (shape[1] > 1 and stride[1] != 1):
         raise PcError("%s: expected [%d, columns] of 32 bits, columns contiguous" % (what, rows))
-    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1]
+    return t.data_ptr(), stride[0] if rows > 1 else shape[1]
 
 
-def _index(t: torch.Tensor, what: str):
-    if t.element_size() != 4 or t.is_floating_point() or t.dim() != 1:
-        raise PcError("%s: expected one dimension of 32-bit integers" % what)
+def _index(t: torch.Tensor, what: str, n: int):
+    if t.dtype not in (torch.int32, torch.uint32) or t.shape != (n,):
+        raise PcError("%s: expected [%d] of 32-bit integers" % (what, n))
     return _ptr(t)
 
 
-def _rows(t: torch.Tensor, what: str, heads: int, dim: int):
+def _rows(t: torch.Tensor, what: str, shape):
     """New tokens [rows, heads, head_dim], head_dim contiguous: (address, row stride, head stride)."""
     if not t.is_cuda:
         raise PcError("expected a GPU tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1:
-        raise PcError("%s: expected [rows, %d, %d], the last dimension contiguous" % (what, heads, dim))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else dim, t.stride(1) if heads > 1 else dim
+    stride = t.stride()
+    if t.shape != shape or stride[2] != 1:
+        raise PcError("%s: expected %s, the last dimension contiguous" % (what, list(shape)))
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[2], stride[1] if shape[1] > 1 else shape[2]
+
+
+def _room(page_table: torch.Tensor, cache, max_kv: Optional[int]) -> int:
+    room = page_table.shape[1] * cache.page_size
+    if max_kv is None:
+        return min(room, _MAX_KV)
+    if not 0 <= max_kv <= room:
+        raise PcError("max_kv: the page table has fewer slots")
+    return max_kv
 
 
 class PagedCache:
@@ -544,23 +566,25 @@ class PagedCache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
+        dtype, shape, stride = _DTYPES.get(k.dtype), k.shape, k.stride()
+        if len(shape) != 4 or v.shape != shape or v.dtype != k.dtype or dtype is None:
             raise PcError("expected two tensors [page, head, slot, head_dim] of bfloat16, float16 or float8_e4m3fn")
         if not (k.is_cuda and v.is_cuda):
             raise PcError("expected a GPU tensor")
-        if k.stride(3) != 1 or any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1):
+        if stride[3] != 1 or (v.stride() != stride and any(a != b for a, b, n in zip(stride, v.stride(), shape) if n > 1)):
             raise PcError("expected equal strides of k and v, head_dim contiguous")
+        if (k_scale is None) != (dtype != 2) or (v_scale is None) != (dtype != 2):
+            raise PcError("k_scale and v_scale go with float8_e4m3fn")
         for x in (k_scale, v_scale):
-            if x is not None and (x.dtype != torch.float32 or x.numel() != k.shape[1]):
+            if x is not None and (x.dtype != torch.float32 or x.shape != shape[1:2]):
                 raise PcError("expected one float32 scale per head")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        size = [s if n > 1 else self.head_dim for s, n in zip(k.stride(), k.shape)]
-        self._c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), size[0], size[1], size[2],
-                           _DTYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
-
-    def _ref(self):
-        return ctypes.addressof(self._c)
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
+        if 1 in shape:   # the stride of a dimension of one is anything
+            stride = [s if n > 1 else self.head_dim for s, n in zip(stride, shape)]
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), stride[0], stride[1], stride[2],
+                           dtype, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
+        self._at = ctypes.addressof(self._c)
 
 
 def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, q_off: torch.Tensor,
@@ -568,20 +592,19 @@ def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor,
     """pc_kv_append: rows q_off[s] .. q_off[s + 1] - 1 of ``k`` and ``v`` ([rows, head,
     head_dim]) into the last slots of the kv_len[s] of sequence s."""
     L = lib()
-    n_seqs = kv_len.numel()
+    n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
-    if max_kv is None:
-        max_kv = min(page_table.shape[1] * cache.page_size, 0x7FFF0000)
-    if k.dtype != v.dtype or k.dtype not in _DTYPES or k.shape != v.shape or q_off.numel() != n_seqs + 1:
-        raise PcError("expected k and v of one shape and type, and one offset more than sequences")
-    if max_kv > page_table.shape[1] * cache.page_size:
-        raise PcError("max_kv: the page table has fewer slots")
-    ka, kr, kh = _rows(k, "k", cache.n_kv_heads, cache.head_dim)
-    va, vr, vh = _rows(v, "v", cache.n_kv_heads, cache.head_dim)
+    max_kv = _room(page_table, cache, max_kv)
+    dtype = _DTYPES.get(k.dtype)
+    if dtype is None or v.dtype != k.dtype:
+        raise PcError("expected k and v of one type, bfloat16 or float16")
+    shape = (k.shape[0], cache.n_kv_heads, cache.head_dim)
+    ka, kr, kh = _rows(k, "k", shape)
+    va, vr, vh = _rows(v, "v", shape)
     if ws is None:
-        ws = workspace(L.pc_kv_append_ws())
-    check(L.pc_kv_append(cache._ref(), table, stride, _index(kv_len, "kv_len"), _index(q_off, "q_off"), n_seqs,
-                         k.shape[0], max_kv, ka, kr, kh, va, vr, vh, _DTYPES[k.dtype], _ptr(ws), ws.numel(), _stream()))
+        ws = _scratch(L.pc_kv_append_ws(), k)
+    check(L.pc_kv_append(cache._at, table, stride, _index(kv_len, "kv_len", n_seqs), _index(q_off, "q_off", n_seqs + 1),
+                         n_seqs, shape[0], max_kv, ka, kr, kh, va, vr, vh, dtype, _ptr(ws), ws.numel(), _stream_of(k)))
     return ws
 
 
@@ -598,47 +621,41 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_
     ([sequence, kv head, max_kv] float32) are formed when ``weight`` or ``weight_out``
     is given."""
     L = lib()
-    n_seqs = kv_len.numel()
+    n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
-    if q.dim() != 3 or q.dtype not in _DTYPES or q_off.numel() != n_seqs + 1:
-        raise PcError("expected q as [rows, heads, head_dim], and one offset more than sequences")
-    n_rows, n_heads, dim = q.shape
-    if dim != cache.head_dim:
-        raise PcError("q: the cache's head_dim is %d" % cache.head_dim)
-    if max_kv is None:
-        max_kv = min(page_table.shape[1] * cache.page_size, 0x7FFF0000)
-    if max_kv > page_table.shape[1] * cache.page_size:
-        raise PcError("max_kv: the page table has fewer slots")
+    max_kv = _room(page_table, cache, max_kv)
+    dtype, shape, device = _DTYPES.get(q.dtype), q.shape, q.device
+    if len(shape) != 3 or dtype is None or shape[2] != cache.head_dim:
+        raise PcError("expected q as [rows, heads, %d] of bfloat16 or float16" % cache.head_dim)
+    n_rows, n_heads, dim = shape
+    qa, qr, qh = _rows(q, "q", shape)
     if out is None:
-        out = torch.empty((n_rows, n_heads, dim), dtype=q.dtype, device=q.device)
-    if out.dtype != q.dtype or out.shape[0] != n_rows:
-        raise PcError("out: expected q's type and rows")
+        out = torch.empty(shape, dtype=q.dtype, device=device)
+        oa, o_r, oh = out.data_ptr(), n_heads * dim, dim
+    else:
+        if out.dtype != q.dtype:
+            raise PcError("out: expected q's type")
+        oa, o_r, oh = _rows(out, "out", shape)
     if lse is None and want_lse:
-        lse = torch.empty((n_rows, n_heads), dtype=torch.float32, device=q.device)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n_rows, n_heads)):
+        lse = torch.empty((n_rows, n_heads), dtype=torch.float32, device=device)
+    elif lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_rows, n_heads)):
         raise PcError("lse: expected [rows, heads] float32")
-    if weight_out is None and weight is not None:
-        weight_out = torch.empty((n_seqs, cache.n_kv_heads, max_kv), dtype=torch.float32, device=q.device)
-    strides = set()
-    for name, w in (("weight", weight), ("weight_out", weight_out)):
-        if w is None:
-            continue
-        if w.dtype != torch.float32 or tuple(w.shape[:2]) != (n_seqs, cache.n_kv_heads) or w.dim() != 3 or \
-                w.shape[2] < max_kv:
-            raise PcError("%s: expected [sequences, kv heads, at least max_kv] float32" % name)
-        _ptr(w)
-        strides.add(w.shape[2])
-    if len(strides) > 1:
-        raise PcError("weight and weight_out: expected one shape")
-    qa, qr, qh = _rows(q, "q", n_heads, dim)
-    oa, o_r, oh = _rows(out, "out", n_heads, dim)
+    weight_stride = 0
+    if weight is not None or weight_out is not None:
+        if weight_out is None:
+            weight_out = torch.empty_like(weight)
+        weight_stride = weight_out.shape[-1]
+        for name, w in (("weight", weight), ("weight_out", weight_out)):
+            if w is not None and (w.dtype != torch.float32 or w.shape != (n_seqs, cache.n_kv_heads, weight_stride) or
+                                  weight_stride < max_kv):
+                raise PcError("%s: expected [sequences, kv heads, at least max_kv] float32" % name)
     if ws is None:
-        ws = workspace(L.pc_attn_paged_ws(n_seqs, n_rows, max_q, max_kv, n_heads, cache.n_kv_heads, dim,
-                                          1 if weight_out is not None else 0))
-    check(L.pc_attn_paged(cache._ref(), table, stride, _index(kv_len, "kv_len"), _index(q_off, "q_off"), n_seqs, n_rows,
-                          max_q, max_kv, qa, qr, qh, _DTYPES[q.dtype], n_heads, dim ** -0.5 if scale is None else scale,
-                          1 if causal else 0, window, oa, o_r, oh, _ptr(lse), _ptr(weight), _ptr(weight_out),
-                          strides.pop() if strides else 0, _ptr(ws), ws.numel(), _stream()))
+        ws = _scratch(L.pc_attn_paged_ws(n_seqs, n_rows, max_q, max_kv, n_heads, cache.n_kv_heads, dim,
+                                         1 if weight_out is not None else 0), q)
+    check(L.pc_attn_paged(cache._at, table, stride, _index(kv_len, "kv_len", n_seqs), _index(q_off, "q_off", n_seqs + 1),
+                          n_seqs, n_rows, max_q, max_kv, qa, qr, qh, dtype, n_heads,
+                          dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, oa, o_r, oh, _ptr(lse),
+                          _ptr(weight), _ptr(weight_out), weight_stride, _ptr(ws), ws.numel(), _stream_of(q)))
     return out, lse, weight_out, ws
 
 
@@ -646,36 +663,42 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
              recent: int, dst_table: Optional[torch.Tensor] = None, max_kv: Optional[int] = None,
              out: Optional[dict] = None, ws: Optional[torch.Tensor] = None):
     """pc_kv_evict: per (sequence, head) the last ``recent`` slots and those of the
-    largest ``weight`` ([sequence, kv head, max_kv] float32), ``budget`` in all, in slot order.
+    largest ``weight`` ([sequence, kv head, at least max_kv] float32), ``budget`` in all, in slot order.
     Their keys and values move to the pages of ``dst_table`` when it is given.  Returns
     {"kept" (int32, -1 behind the last), "weight", "new_len", "ws"}."""
     L = lib()
-    n_seqs = kv_len.numel()
+    n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
-    if weight.dtype != torch.float32 or weight.dim() != 3 or tuple(weight.shape[:2]) != (n_seqs, cache.n_kv_heads):
+    heads, device = cache.n_kv_heads, weight.device
+    if weight.dtype != torch.float32 or len(weight.shape) != 3 or weight.shape[:2] != (n_seqs, heads):
         raise PcError("weight: expected [sequences, kv heads, slots] float32")
     if max_kv is None:
         max_kv = min(page_table.shape[1] * cache.page_size, weight.shape[2])
-    if max_kv > page_table.shape[1] * cache.page_size or max_kv > weight.shape[2]:
-        raise PcError("max_kv: the page table or the weights have fewer slots")
-    dst, dst_stride = (None, 0) if dst_table is None else _table(dst_table, "dst_table", n_seqs)
-    if dst_table is not None and dst_table.shape[1] * cache.page_size < budget:
-        raise PcError("dst_table: room for fewer than budget slots")
-    shape = (n_seqs, cache.n_kv_heads, budget)
+    max_kv = _room(page_table, cache, max_kv)
+    if max_kv > weight.shape[2]:
+        raise PcError("max_kv: the weights have fewer slots")
+    dst, dst_stride = None, 0
+    if dst_table is not None:
+        dst, dst_stride = _table(dst_table, "dst_table", n_seqs)
+        if dst_table.shape[1] * cache.page_size < budget:
+            raise PcError("dst_table: room for fewer than budget slots")
+    shape = (n_seqs, heads, budget)
     if out is None:
-        out = {"kept": torch.empty(shape, dtype=torch.int32, device=weight.device),
-               "weight": torch.empty(shape, dtype=torch.float32, device=weight.device),
-               "new_len": torch.empty(n_seqs, dtype=torch.int32, device=weight.device)}
-    for name in ("kept", "weight"):
-        if out.get(name) is not None and (tuple(out[name].shape) != shape or out[name].element_size() != 4):
-            raise PcError("%s: expected [sequences, kv heads, budget] of 32 bits" % name)
-    if out["new_len"].numel() != n_seqs or out["new_len"].element_size() != 4:
-        raise PcError("new_len: expected one 32-bit integer per sequence")
+        if budget < 1:
+            raise PcError("budget: expected at least 1")
+        out = {"kept": torch.empty(shape, dtype=torch.int32, device=device),
+               "weight": torch.empty(shape, dtype=torch.float32, device=device),
+               "new_len": torch.empty((n_seqs,), dtype=torch.int32, device=device)}
+    else:
+        for name in ("kept", "weight"):
+            x = out.get(name)
+            if (x is None and name == "kept") or (x is not None and (x.shape != shape or x.element_size() != 4)):
+                raise PcError("%s: expected [sequences, kv heads, budget] of 32 bits" % name)
     if ws is None:
-        ws = workspace(L.pc_kv_evict_ws(n_seqs, cache.n_kv_heads, max_kv))
-    check(L.pc_kv_evict(cache._ref(), table, stride, _index(kv_len, "kv_len"), n_seqs, max_kv, _ptr(weight),
+        ws = _scratch(L.pc_kv_evict_ws(n_seqs, heads, max_kv), weight)
+    check(L.pc_kv_evict(cache._at, table, stride, _index(kv_len, "kv_len", n_seqs), n_seqs, max_kv, _ptr(weight),
                         weight.shape[2], budget, recent, dst, dst_stride, _ptr(out["kept"]), _ptr(out.get("weight")),
-                        _ptr(out["new_len"]), _ptr(ws), ws.numel(), _stream()))
+                        _index(out["new_len"], "new_len", n_seqs), _ptr(ws), ws.numel(), _stream_of(weight)))
     out["ws"] = ws
     return out
 

@@ -16,9 +16,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float MINUS_INF = -__builtin_inff();
 
+// A row's weights are exp2(score - ref + TOP), ref a maximum of the scores so far that
+// may lag behind by SLACK: most tiles that bring a slightly larger one need no
+// rescaling of the sums (the factor cancels in sum p v / sum p).
 struct Bf16 {
-    // exp2(score - max) is at most 1
-    static constexpr float TOP = 0.f;
+    static constexpr float TOP = 0.f, SLACK = 8.f;
     static __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
@@ -34,9 +36,8 @@ struct Bf16 {
     static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
 };
 struct F16 {
-    // f16 has five exponent bits: weights down to 2^-29 of the largest stay
-    // normal numbers when that one is 2^15 (the factor cancels in sum p v / sum p)
-    static constexpr float TOP = 15.f;
+    // f16 has five exponent bits: at most 2^15, and down to 2^-25 of ref normal numbers
+    static constexpr float TOP = 11.f, SLACK = 4.f;
     static __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
@@ -83,27 +84,55 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 }
 
 // Keys and values of 16-bit elements lie in LDS as rows of D, in pieces of 16
-// bytes.  A wave reads a column of pieces over consecutive rows (keys) and the
-// same four pieces of four consecutive rows (the transposed reads of values);
-// piece c of row k is at c ^ spread(k), so that both, and writes of whole rows,
-// meet every bank once.
+// bytes.  LDS has 64 banks of 4 bytes: 16 lanes' pieces, or 32 lanes' 8 bytes, at a
+// time.  Keys are read as a column of pieces over 16 consecutive rows, values (transposed) as
+// four neighbouring pieces of four consecutive rows.  Piece c of row k is at c ^ spread(k):
+// both then meet every bank once, and so do writes of whole rows or columns.
 template <int D>
-__device__ __forceinline__ uint32_t spread(uint32_t row) {
-    return ((row & 3) << 1 | (row >> 2 & 1)) & (D / 8 - 1);
+constexpr __device__ __forceinline__ uint32_t spread(uint32_t row) {
+    return D == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
 }
 template <int D>
 __device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
     return row * (D * 2) + ((c ^ spread<D>(row)) * 16);
 }
-// four keys of one value dimension a lane: rows row .. row + 3 of the 16 lanes
-// of each group, dimension 16 * (group & 1) + lane % 16 of the 32 from d0
-template <int D>
-__device__ __forceinline__ uint2 read_transposed(const char *tile, uint32_t row, uint32_t d) {
-    // this lane's address: row and d are those of the four elements that it fetches
+// four keys of one value dimension a lane: the 16 lanes of a group fetch 8 bytes each
+// of four rows of 16 elements and get a column each
+__device__ __forceinline__ uint2 read_transposed(const char *p) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const char *p = tile + piece_at<D>(row, d / 8) + (d % 8) * 2;
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
 }
+// Where this lane fetches values: of the 16 keys at hand, rows 4 half + lane % 16 / 4 (lo) and 8
+// further (hi) of dimensions 32 b + 16 (lane / 16 % 2) + 4 (lane % 4) .. + 3.  The spread has
+// four bits (two pairs of blocks are 256 bytes apart), so a few numbers a lane serve all
+// rows and blocks: at[b % 4] + b / 4 * 256.
+template <int D>
+struct ValueAt {
+    uint32_t lo[D == 64 ? 2 : 4], hi[D == 64 ? 2 : 4];
+    __device__ __forceinline__ ValueAt() {
+        const uint32_t lane = threadIdx.x & (WAVE - 1), row = 4 * (lane / 32) + lane % 16 / 4;
+#pragma unroll
+        for (uint32_t b = 0; b < (D == 64 ? 2 : 4); ++b) {
+            const uint32_t c = 4 * b + 2 * (lane / 16 % 2) + lane % 4 / 2;
+            lo[b] = piece_at<D>(row, c) + lane % 2 * 8;
+            hi[b] = piece_at<D>(row + 8, c) + lane % 2 * 8;
+        }
+    }
+};
+// Where this lane finds its key (or query row) lane % 32 of a tile, step i of its dimensions.
+template <int D>
+struct RowAt {
+    uint32_t at[D == 64 ? 4 : 8];
+    __device__ __forceinline__ RowAt() {
+        const uint32_t lane = threadIdx.x & (WAVE - 1);
+#pragma unroll
+        for (uint32_t i = 0; i < (D == 64 ? 4 : 8); ++i)
+            at[i] = piece_at<D>(lane % 32, 4 * (i / 2) + 2 * (lane / 32) + i % 2);
+    }
+    __device__ __forceinline__ uint4 read(const char *tile, int i) const {
+        return *(const uint4 *)(tile + at[i % (D == 64 ? 4 : 8)] + i / 8 * 256);
+    }
+};
 
 // ------------------------------------------------------------------ arguments
 
@@ -123,6 +152,7 @@ struct AttnArgs {
     FastDiv by_group;
     float scale;
     uint32_t causal, window;
+    uint32_t by_16;              // 16 slots from a multiple of 16 share a page, their strides small
     // the work list
     uint32_t target;             // items wanted
     uint32_t least;              // tiles of an item, at least
@@ -289,7 +319,8 @@ __device__ __forceinline__ void load_query(const AttnArgs &a, const char *row, b
 }
 
 // softmax state of the rows of a wave: lane % 32 is the row; the maximum is
-// common to both halves, the sum is each half's own until the end
+// common to both halves, the sum is each half's own until the end.  Scores are taken
+// times c, and `slack` is SLACK / c.
 template <class T, int D>
 struct Rows {
     f32x16 o[D / 32];
@@ -302,23 +333,22 @@ struct Rows {
     }
     // scores of 32 * B keys -> weights packed as the right operand of O^T += V^T P^T
     template <int B>
-    __device__ __forceinline__ void weigh(f32x16 (&s)[B], float c, uint4 (&p)[2 * B]) {
+    __device__ __forceinline__ void weigh(f32x16 (&s)[B], float c, float slack, uint4 (&p)[2 * B]) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
         top = max_of_halves(top);
-        const float next = fmaxf(m, top);
-        // a row that has seen nothing yet keeps weights of 0: exp2(-inf - 0)
-        const float ref = next == MINUS_INF ? 0.f : next;
-        if (ballot(next > m)) {
-            const float f = exp2_fast((m - ref) * c);
+        if (ballot(top > m + slack)) {
+            // a row that has seen nothing keeps a sum of 0: exp2(-inf - 0)
+            const float next = fmaxf(m, top), f = exp2_fast((m - (next == MINUS_INF ? 0.f : next)) * c);
             l *= f;
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) o[b] *= f;
             m = next;
         }
+        const float ref = m == MINUS_INF ? 0.f : m;
         const float shift = T::TOP - ref * c;
         float sum = 0.f;
 #pragma unroll
@@ -334,14 +364,12 @@ struct Rows {
         }
         l += sum;
     }
-    // O^T += V^T P^T over 16 keys from row k0 of the tile
-    __device__ __forceinline__ void add(const char *v, uint32_t k0, uint4 p) {
-        const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32, row = k0 + 4 * half + lane % 16 / 4;
-        const uint32_t d = (lane / 16 % 2) * 16 + (lane % 4) * 4;
+    // O^T += V^T P^T over 16 keys, the first of them at `v`
+    __device__ __forceinline__ void add(const char *v, const ValueAt<D> &at, uint4 p) {
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) {
-            const uint2 x = read_transposed<D>(v, row, 32 * b + d), y = read_transposed<D>(v, row + 8, 32 * b + d);
-            o[b] = T::mfma(make_uint4(x.x, x.y, y.x, y.y), p, o[b]);
+            const uint2 lo = read_transposed(v + at.lo[b % 4] + b / 4 * 256), hi = read_transposed(v + at.hi[b % 4] + b / 4 * 256);
+            o[b] = T::mfma(make_uint4(lo.x, lo.y, hi.x, hi.y), p, o[b]);
         }
     }
 };

@@ -16,22 +16,17 @@ __device__ __forceinline__ uint64_t entry_at(const KvView &kv, uint32_t page, ui
 // a table entry that does not fit reads page 0 (the join reports it)
 __device__ __forceinline__ uint32_t page_of(const KvView &kv, uint32_t entry) { return entry < kv.n_pages ? entry : 0; }
 
+// x with the elements that are not finite zeroed; *any is set if there are any
 template <class T>
-__device__ __forceinline__ bool not_finite(uint32_t w) {
-    return (w & T::EXPONENT) == T::EXPONENT || (w >> 16 & T::EXPONENT) == T::EXPONENT;
+__device__ __forceinline__ uint32_t drop_not_finite(uint32_t w, bool *any) {
+    const bool lo = (w & T::EXPONENT) == T::EXPONENT, hi = (w >> 16 & T::EXPONENT) == T::EXPONENT;
+    *any |= lo | hi;
+    return (lo ? 0 : w & 0xFFFFu) | (hi ? 0 : w & 0xFFFF0000u);
 }
-// zeroes the elements that are not finite; says whether there were any
 template <class T>
-__device__ __forceinline__ bool drop_not_finite(uint4 *x) {
-    uint32_t w[4] = {x->x, x->y, x->z, x->w};
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((w[i] & T::EXPONENT) == T::EXPONENT) { w[i] &= 0xFFFF0000u; any = true; }
-        if ((w[i] >> 16 & T::EXPONENT) == T::EXPONENT) { w[i] &= 0xFFFFu; any = true; }
-    }
-    *x = make_uint4(w[0], w[1], w[2], w[3]);
-    return any;
+__device__ __forceinline__ uint4 drop_not_finite(uint4 x, bool *any) {
+    return make_uint4(drop_not_finite<T>(x.x, any), drop_not_finite<T>(x.y, any), drop_not_finite<T>(x.z, any),
+                      drop_not_finite<T>(x.w, any));
 }
 
 // Values that are not finite, in tiles whose keys some rows see and some do not: the
@@ -186,12 +181,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         *(uint4 *)(queries + piece_at<D>((threadIdx.x + 256 * i) / (D / 8), threadIdx.x % (D / 8))) = q[i];
     __syncthreads();
     bool odd = false;   // a value that is not finite was left out of a tile
-    auto query = [&](int i) { return *(const uint4 *)(queries + piece_at<D>(col, dim_of_step(i, half) / 8)); };
+    const RowAt<D> q_at;
+    const ValueAt<D> v_at;
+    const float slack = T::SLACK / c;
+    auto query = [&](int i) { return q_at.read(queries, i); };
     for (; t < t_end; t += 4) {
         const bool more = t + 4 < t_end;
         const uint32_t k0 = it.shape.keys.lo + t * 32;
         const bool full = (int32_t)k0 >= all_first && (int32_t)k0 + 31 <= all_last;
-        f32x16 s[1] = {f32x16(0.f)};
+        f32x16 s[1];
         if (!FULL) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
@@ -202,9 +200,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
             if (F8) {
                 uint4 x, y;
                 expand<T>(k[i / 2], &x, &y);
-                s[0] = T::mfma(i % 2 ? y : x, query(i), s[0]);
+                s[0] = T::mfma(i % 2 ? y : x, query(i), i ? s[0] : f32x16(0.f));
             } else {
-                s[0] = T::mfma(k[i % PIECES], query(i), s[0]);
+                s[0] = T::mfma(k[i % PIECES], query(i), i ? s[0] : f32x16(0.f));
             }
         }
         if (more) {
@@ -214,12 +212,17 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t n = F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
-            uint4 x[2] = {v[i], v[i]};
-            if (F8) expand<T>(v[i], &x[0], &x[1]);
-#pragma unroll
-            for (int e = 0; e < (F8 ? 2 : 1); ++e) {
-                if (!full) odd |= drop_not_finite<T>(&x[e]);
-                *(uint4 *)(tile + piece_at<D>(col, n + e)) = x[e];
+            auto put = [&](uint4 x, int e) {
+                if (!full) x = drop_not_finite<T>(x, &odd);
+                *(uint4 *)(tile + piece_at<D>(col, n + e)) = x;
+            };
+            if (F8) {
+                uint4 x, y;
+                expand<T>(v[i], &x, &y);
+                put(x, 0);
+                put(y, 1);
+            } else {
+                put(v[i], 0);
             }
         }
         if (more) {
@@ -240,11 +243,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
                 *(float4 *)(w + 2 * r) = make_float4(s[0][r] * c, s[0][r + 1] * c, s[0][r + 2] * c, s[0][r + 3] * c);
         }
         uint4 p[2];
-        state.template weigh<1>(s, c, p);
+        state.template weigh<1>(s, c, slack, p);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        state.add(tile, 0, p[0]);
-        state.add(tile, 16, p[1]);
+        state.add(tile, v_at, p[0]);
+        state.add(tile + 16 * D * 2, v_at, p[1]);
         __builtin_amdgcn_wave_barrier();
     }
     if (ballot(odd)) {
@@ -347,8 +350,18 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
 
     uint4 k[PIECES], v[PIECES];
+    // Where a page holds whole groups of 16 slots, a wave's rows of a piece lie in one group and
+    // its address is one number for the wave: the table's entries are read 64 groups at a time,
+    // a lane each, and the arithmetic is scalar.  Else every thread finds its rows' pages.
+    const uint32_t n_piece = tid % PER_ROW;
+    const bool past_dim = !FULL && n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
+    const uint32_t o_piece = past_dim ? 0 : n_piece * 16, o_lane = lane / PER_ROW * (uint32_t)a.kv.st + o_piece;
+    const uint32_t g_last = (k_hi - 1) / 16;
+    uint32_t groups = 0, groups_next = 0, g0 = k_lo / 16;   // entries of groups g0 + lane, g0 + 64 + lane
     uint32_t entry[PIECES], off[PIECES];
+    auto look_up_groups = [&](uint32_t g) { return table[a.kv.by_page.div(min(g + lane, g_last) * 16)]; };
     auto look_up = [&](uint32_t k0) {
+        if (a.by_16) return;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t j = min(k0 + (tid + 256 * i) / PER_ROW, k_hi - 1), p = a.kv.by_page.div(j);
@@ -356,10 +369,24 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
             entry[i] = table[p];
         }
     };
-    const uint32_t n_piece = tid % PER_ROW;
-    const bool past_dim = !FULL && n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
-    const uint32_t o_piece = past_dim ? 0 : n_piece * 16;
-    auto load = [&]() {
+    auto load = [&](uint32_t k0) {
+        if (a.by_16) {
+            if (k0 / 16 - g0 >= WAVE) {
+                g0 += WAVE;
+                groups = groups_next;
+                groups_next = look_up_groups(g0 + WAVE);
+            }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t r = (wave * WAVE + 256 * i) / PER_ROW, g = min(k0 / 16 + r / 16, g_last), slot = g * 16;
+                const uint32_t p = a.kv.by_page.div(slot);
+                const uint32_t page = page_of(a.kv, from_lane(groups, (int)(g - g0)));
+                const uint64_t at = entry_at(a.kv, page, slot - p * a.kv.page + r % 16, it.head);
+                k[i] = *(const uint4 *)(a.kv.k + at + o_lane);
+                v[i] = *(const uint4 *)(a.kv.v + at + o_lane);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint64_t at = entry_at(a.kv, page_of(a.kv, entry[i]), off[i], it.head) + o_piece;
@@ -372,52 +399,68 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     };
     if (tid == 0) odd = 0;
     __syncthreads();
-    auto store = [&](int buf, bool edge) {
+    uint32_t to[F8 ? 2 : 1];   // this thread's places in a tile
+#pragma unroll
+    for (int e = 0; e < (F8 ? 2 : 1); ++e) to[e] = piece_at<D>(tid / PER_ROW, n_piece * (F8 ? 2 : 1) + e);
+    auto store = [&](int buf, uint32_t k0) {
+        const bool edge = is_edge(k0);
         bool mine = false;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t r = (tid + 256 * i) / PER_ROW;
-            if (past_dim) k[i] = make_uint4(0, 0, 0, 0);
-            uint4 x[2] = {k[i], k[i]}, y[2] = {v[i], v[i]};
+            // rows a multiple of 16 on have the same spread, those 8 on another by 2
+            const uint32_t at = 256 / PER_ROW * i * D * 2, turn = 256 / PER_ROW == 8 && i % 2 ? 32 : 0;
+            auto put = [&](uint4 x, uint4 y, int e) {
+                if (past_dim) x = make_uint4(0, 0, 0, 0);
+                if (edge) {   // slots past the end may hold anything
+                    if (k0 + (tid + 256 * i) / PER_ROW >= k_hi) y = make_uint4(0, 0, 0, 0);
+                    y = drop_not_finite<T>(y, &mine);
+                }
+                const uint32_t o = (to[e] ^ turn) + at;
+                *(uint4 *)(lds[buf][0] + o) = x;
+                *(uint4 *)(lds[buf][1] + o) = y;
+            };
             if (F8) {
-                expand<T>(k[i], &x[0], &x[1]);
-                expand<T>(v[i], &y[0], &y[1]);
-            }
-#pragma unroll
-            for (int e = 0; e < (F8 ? 2 : 1); ++e) {
-                const uint32_t at = piece_at<D>(r, n_piece * (F8 ? 2 : 1) + e);
-                if (edge) mine |= drop_not_finite<T>(&y[e]);
-                *(uint4 *)(lds[buf][0] + at) = x[e];
-                *(uint4 *)(lds[buf][1] + at) = y[e];
+                uint4 x0, x1, y0, y1;
+                expand<T>(k[i], &x0, &x1);
+                expand<T>(v[i], &y0, &y1);
+                put(x0, y0, 0);
+                put(x1, y1, F8 ? 1 : 0);
+            } else {
+                put(k[i], v[i], 0);
             }
         }
         if (mine) odd = 1;
     };
+    const RowAt<D> k_at;
+    const ValueAt<D> v_at;
+    const float slack = T::SLACK / c;
     Rows<T, D> state;
     state.clear();
     if (k_lo < k_hi) {
+        if (a.by_16) {
+            groups = look_up_groups(g0);
+            groups_next = look_up_groups(g0 + WAVE);
+        }
         look_up(k_lo);
-        load();
+        load(k_lo);
         if (k_lo + CHUNK_KEYS < k_hi) look_up(k_lo + CHUNK_KEYS);
-        store(0, is_edge(k_lo));
+        store(0, k_lo);
         __syncthreads();
     }
     int buf = 0;
     for (uint32_t k0 = k_lo; k0 < k_hi; k0 += CHUNK_KEYS) {
         const uint32_t next = k0 + CHUNK_KEYS;
         if (next < k_hi) {
-            load();
+            load(next);
             if (next + CHUNK_KEYS < k_hi) look_up(next + CHUNK_KEYS);
         }
         const char *kt = lds[buf][0], *vt = lds[buf][1];
         f32x16 s[BLOCKS];
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) s[b] = f32x16(0.f);
-#pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-                s[b] = T::mfma(*(const uint4 *)(kt + piece_at<D>(32 * b + col, dim_of_step(i, half) / 8)), q[i], s[b]);
+                s[b] = T::mfma(k_at.read(kt + 32 * b * D * 2, i), q[i], i ? s[b] : f32x16(0.f));
         if ((int32_t)k0 < all_first || (int32_t)(k0 + CHUNK_KEYS - 1) > all_last || next > k_hi) {
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
@@ -428,10 +471,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
                 }
         }
         uint4 p[2 * BLOCKS];
-        state.template weigh<BLOCKS>(s, c, p);
+        state.template weigh<BLOCKS>(s, c, slack, p);
 #pragma unroll
-        for (int t = 0; t < 2 * BLOCKS; ++t) state.add(vt, 16 * t, p[t]);
-        if (next < k_hi) store(buf ^ 1, is_edge(next));
+        for (int t = 0; t < 2 * BLOCKS; ++t) state.add(vt + 16 * t * D * 2, v_at, p[t]);
+        if (next < k_hi) store(buf ^ 1, next);
         __syncthreads();
         buf ^= 1;
     }
@@ -508,45 +551,46 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
         const uint32_t tile = blockIdx.x / row_blocks;
         const Item it = find_item<By::TILE>(a, tile);
         if (!it.there || it.splits < 2) return;
-        const uint32_t at = tid / LANES, lane = tid % LANES, team = at % teams;
-        const uint32_t row = (blockIdx.x - tile * row_blocks) * (ALL / teams) + at / teams;   // of the tile
-        const uint32_t r = it.row_tile * a.row_tile + row;
-        const bool there = row < a.row_tile && r < it.shape.q.rows * a.group;
-        if ((blockIdx.x - tile * row_blocks) * (ALL / teams) + it.row_tile * a.row_tile >= it.shape.q.rows * a.group) return;
-        const uint32_t rr = there ? row : 0;
-        const float2 ml = join_stats(a, it, it.head, it.row_tile, rr, lane, LANES);
-        const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t p = team; p < it.splits; p += teams) {
-            const uint32_t slot = slot_of(a, it, it.head, it.row_tile, p);
-            if (slot >= a.slots) continue;
-            const uint64_t i = (uint64_t)slot * a.slot_rows + rr;
-            const float m = a.part_ml[i].x;
-            if (m == MINUS_INF) continue;
-            const float4 x = *(const float4 *)(a.part + i * D + lane * 4);
-            const float f = exp2_fast(m - ref);
-            sum = make_float4(sum.x + x.x * f, sum.y + x.y * f, sum.z + x.z * f, sum.w + x.w * f);
+        const uint32_t at = tid / LANES, lane = tid % LANES, team = at % teams, step = ALL / teams;
+        const uint32_t r0 = it.row_tile * a.row_tile, rows = min(a.row_tile, it.shape.q.rows * a.group - r0);
+        for (uint32_t from = (blockIdx.x - tile * row_blocks) * step; from < rows; from += row_blocks * step) {
+            const bool there = from + at / teams < rows;
+            const uint32_t row = there ? from + at / teams : from;
+            const float2 ml = join_stats(a, it, it.head, it.row_tile, row, lane, LANES);
+            const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (uint32_t p = team; p < it.splits; p += teams) {
+                const uint32_t slot = slot_of(a, it, it.head, it.row_tile, p);
+                if (slot >= a.slots) continue;
+                const uint64_t i = (uint64_t)slot * a.slot_rows + row;
+                const float m = a.part_ml[i].x;
+                if (m == MINUS_INF) continue;
+                const float4 x = *(const float4 *)(a.part + i * D + lane * 4);
+                const float f = exp2_fast(m - ref);
+                sum = make_float4(sum.x + x.x * f, sum.y + x.y * f, sum.z + x.z * f, sum.w + x.w * f);
+            }
+            if (teams > 1) {
+                __syncthreads();
+                sums[tid] = sum;
+                __syncthreads();
+            }
+            if (team || !there) continue;
+            for (uint32_t i = 1; i < teams; ++i) {
+                const float4 x = sums[tid + i * LANES];
+                sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+            }
+            const bool none = ml.x == MINUS_INF;
+            const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / ml.y;
+            const float base2 = none ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+            const uint32_t i = a.by_group.div(r0 + row), t = it.shape.q.first + i, e = it.head * a.group + (r0 + row - i * a.group);
+            if (lane == 0) {
+                if (a.lse) a.lse[(uint64_t)t * a.n_heads + e] = base2 * LN2;
+                if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + e] = base2;
+            }
+            if (lane * 4 < a.kv.dim)
+                *(uint2 *)(a.out + (uint64_t)t * a.o_row + e * a.o_head + lane * 8) =
+                    make_uint2(T::pack(sum.x * f, sum.y * f), T::pack(sum.z * f, sum.w * f));
         }
-        if (teams > 1) {
-            sums[tid] = sum;
-            __syncthreads();
-        }
-        if (team || !there) return;
-        for (uint32_t i = 1; i < teams; ++i) {
-            const float4 x = sums[tid + i * LANES];
-            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
-        }
-        const bool none = ml.x == MINUS_INF;
-        const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / ml.y;
-        const float base2 = none ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
-        const uint32_t i = a.by_group.div(r), t = it.shape.q.first + i, e = it.head * a.group + (r - i * a.group);
-        if (lane == 0) {
-            if (a.lse) a.lse[(uint64_t)t * a.n_heads + e] = base2 * LN2;
-            if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + e] = base2;
-        }
-        if (lane * 4 < a.kv.dim)
-            *(uint2 *)(a.out + (uint64_t)t * a.o_row + e * a.o_head + lane * 8) =
-                make_uint2(T::pack(sum.x * f, sum.y * f), T::pack(sum.z * f, sum.w * f));
         return;
     }
     // weights of WEIGH_KEYS keys of one (sequence, head) from the scores
@@ -647,6 +691,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
             }
         }
         const uint32_t n_piece = tid % (D / 8);
+        const RowAt<D> q_at;
         uint4 x[PIECES];
         float base = 0.f;
         int32_t place = 0;
@@ -696,12 +741,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
                               w_last >= (int32_t)k_hi;
 #pragma unroll
             for (int m = 0; m < WEIGHT_ROWS / 32; ++m) {
-                f32x16 z[2] = {f32x16(0.f), f32x16(0.f)};
+                f32x16 z[2];
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    const uint4 y = *(const uint4 *)(lds[buf] + piece_at<D>(32 * m + col, dim_of_step(i, half) / 8));
+                    const uint4 y = q_at.read(lds[buf] + 32 * m * D * 2, i);
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) z[n] = T::mfma(y, k[n][i], z[n]);
+                    for (int n = 0; n < 2; ++n) z[n] = T::mfma(y, k[n][i], i ? z[n] : f32x16(0.f));
                 }
                 float g[2] = {0.f, 0.f};
 #pragma unroll
@@ -820,11 +865,13 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, 
     } else {
         PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL>), items, dim3(256), 0, st, a);
     }
-    // few joins take several teams to a row
+    // few joins take several teams to a row; many are walked by at most 2048 workgroups, or one
+    // a tile (most of them find whole results and end)
     constexpr uint32_t ALL = 256 / (D / 4);
     uint32_t teams = ALL;
     while (teams > 1 && tiles * p.slot_rows * teams / ALL > 4096) teams /= 2;
-    const uint32_t row_blocks = (p.slot_rows * teams + ALL - 1) / ALL;
+    uint32_t row_blocks = (p.slot_rows * teams + ALL - 1) / ALL;
+    while (row_blocks > 1 && tiles * row_blocks > 2048) row_blocks = (row_blocks + 1) / 2;
     const uint32_t key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
     const uint64_t joins = tiles * row_blocks;
     const uint64_t weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * key_blocks : 0;
@@ -911,6 +958,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.scale = scale;
     a.causal = flags & PC_ATTN_CAUSAL;
     a.window = window;
+    a.by_16 = a.kv.page % 16 == 0 && a.kv.st < (1u << 24);
     a.target = p.few ? ROWS_ITEMS : CHUNK_ITEMS;
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;

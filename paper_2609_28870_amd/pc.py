@@ -520,7 +520,7 @@ def _stream_of(t: torch.Tensor):
 
 
 def _scratch(nbytes: int, t: torch.Tensor) -> torch.Tensor:
-    return torch.empty(nbytes, dtype=torch.uint8, device=t.device)
+    return t.new_empty((nbytes,), dtype=torch.uint8)
 
 
 def _table(t: torch.Tensor, what: str, rows: int):
@@ -624,20 +624,20 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_
     n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
     max_kv = _room(page_table, cache, max_kv)
-    dtype, shape, device = _DTYPES.get(q.dtype), q.shape, q.device
+    dtype, shape = _DTYPES.get(q.dtype), q.shape
     if len(shape) != 3 or dtype is None or shape[2] != cache.head_dim:
         raise PcError("expected q as [rows, heads, %d] of bfloat16 or float16" % cache.head_dim)
     n_rows, n_heads, dim = shape
     qa, qr, qh = _rows(q, "q", shape)
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=device)
+        out = q.new_empty(shape)
         oa, o_r, oh = out.data_ptr(), n_heads * dim, dim
     else:
         if out.dtype != q.dtype:
             raise PcError("out: expected q's type")
         oa, o_r, oh = _rows(out, "out", shape)
     if lse is None and want_lse:
-        lse = torch.empty((n_rows, n_heads), dtype=torch.float32, device=device)
+        lse = q.new_empty((n_rows, n_heads), dtype=torch.float32)
     elif lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_rows, n_heads)):
         raise PcError("lse: expected [rows, heads] float32")
     weight_stride = 0
@@ -669,7 +669,7 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
     L = lib()
     n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
-    heads, device = cache.n_kv_heads, weight.device
+    heads = cache.n_kv_heads
     if weight.dtype != torch.float32 or len(weight.shape) != 3 or weight.shape[:2] != (n_seqs, heads):
         raise PcError("weight: expected [sequences, kv heads, slots] float32")
     if max_kv is None:
@@ -686,9 +686,8 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
     if out is None:
         if budget < 1:
             raise PcError("budget: expected at least 1")
-        out = {"kept": torch.empty(shape, dtype=torch.int32, device=device),
-               "weight": torch.empty(shape, dtype=torch.float32, device=device),
-               "new_len": torch.empty((n_seqs,), dtype=torch.int32, device=device)}
+        out = {"kept": weight.new_empty(shape, dtype=torch.int32), "weight": weight.new_empty(shape),
+               "new_len": kv_len.new_empty((n_seqs,))}
     else:
         for name in ("kept", "weight"):
             x = out.get(name)

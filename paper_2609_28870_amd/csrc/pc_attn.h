@@ -242,51 +242,56 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
     const uint64_t len = (tiles * a.kv.n_kv + a.target - 1) / a.target;
     it.length = uniform(len > a.least ? (uint32_t)(len < 0x7FFFFFFFu ? len : 0x7FFFFFFFu) : a.least);
     uint64_t base = 0, slot = 0;
-    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
-        const uint32_t s = s0 + lane;
-        uint32_t items = 0, splits = 1, count = 0;
-        if (s < a.n_seqs) {
-            if (a.n_seqs > WAVE) h = shape_of(a, s);
-            splits = (h.key_tiles + it.length - 1) / it.length;
-            splits = splits ? splits : 1;
-            const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
-            items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
-            count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
-        }
-        const uint32_t partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
-        const uint32_t end = BY == By::SEQ ? 0 : wave_incl_scan(count);
-        int at;
-        if (BY == By::SEQ) at = key - s0 < WAVE ? (int)(key - s0) : WAVE;
-        else at = __popcll(ballot(base + end <= key));
-        at = (int)uniform((uint32_t)at);
-        if (at < WAVE && s0 + at < a.n_seqs) {
-            it.there = true;
-            it.seq = s0 + at;
-            it.splits = from_lane(splits, at);
-            it.shape.q.first = from_lane(h.q.first, at);
-            it.shape.q.rows = from_lane(h.q.rows, at);
-            it.shape.q.len = from_lane(h.q.len, at);
-            it.shape.keys.lo = from_lane(h.keys.lo, at);
-            it.shape.keys.hi = from_lane(h.keys.hi, at);
-            it.shape.row_tiles = from_lane(h.row_tiles, at);
-            it.shape.key_tiles = from_lane(h.key_tiles, at);
-            it.slot = (uint32_t)slot + from_lane(slot_end - partial, at);
-            it.head = it.row_tile = it.split = 0;
-            if (BY != By::SEQ) {
-                // heads first (neighbouring workgroups are on different XCDs, so with 2, 4 or 8
-                // heads an L2 holds one or few heads' keys), then rows, the last ones first
-                // (they see the most keys), then ranges
-                const uint32_t i = key - (uint32_t)(base + from_lane(end - count, at));
-                const uint32_t j = i / a.kv.n_kv;
-                it.head = i - j * a.kv.n_kv;
-                it.split = j / it.shape.row_tiles;
-                it.row_tile = it.shape.row_tiles - 1 - (j - it.split * it.shape.row_tiles);
-                if (BY == By::ITEM) it.slot += i;
+    // the ranges of the sequences that are cut come first: what is left for the end is smaller
+    const int classes = BY == By::SEQ ? 1 : 2;
+#pragma unroll 1
+    for (int whole = 0; whole < classes; ++whole) {
+        for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
+            const uint32_t s = s0 + lane;
+            uint32_t items = 0, splits = 1, count = 0;
+            if (s < a.n_seqs) {
+                if (a.n_seqs > WAVE) h = shape_of(a, s);
+                splits = (h.key_tiles + it.length - 1) / it.length;
+                splits = splits ? splits : 1;
+                const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
+                items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
+                if ((splits == 1) == (whole == 1)) count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
             }
-            return it;
+            const uint32_t partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
+            const uint32_t end = BY == By::SEQ ? 0 : wave_incl_scan(count);
+            int at;
+            if (BY == By::SEQ) at = key - s0 < WAVE ? (int)(key - s0) : WAVE;
+            else at = __popcll(ballot(base + end <= key));
+            at = (int)uniform((uint32_t)at);
+            if (at < WAVE && s0 + at < a.n_seqs) {
+                it.there = true;
+                it.seq = s0 + at;
+                it.splits = from_lane(splits, at);
+                it.shape.q.first = from_lane(h.q.first, at);
+                it.shape.q.rows = from_lane(h.q.rows, at);
+                it.shape.q.len = from_lane(h.q.len, at);
+                it.shape.keys.lo = from_lane(h.keys.lo, at);
+                it.shape.keys.hi = from_lane(h.keys.hi, at);
+                it.shape.row_tiles = from_lane(h.row_tiles, at);
+                it.shape.key_tiles = from_lane(h.key_tiles, at);
+                it.slot = (uint32_t)slot + from_lane(slot_end - partial, at);
+                it.head = it.row_tile = it.split = 0;
+                if (BY != By::SEQ) {
+                    // heads first (neighbouring workgroups are on different XCDs, so with 2, 4 or 8
+                    // heads an L2 holds one or few heads' keys), then rows, the last ones first
+                    // (they see the most keys), then ranges
+                    const uint32_t i = key - (uint32_t)(base + from_lane(end - count, at));
+                    const uint32_t j = i / a.kv.n_kv;
+                    it.head = i - j * a.kv.n_kv;
+                    it.split = j / it.shape.row_tiles;
+                    it.row_tile = it.shape.row_tiles - 1 - (j - it.split * it.shape.row_tiles);
+                    if (BY == By::ITEM) it.slot += i;
+                }
+                return it;
+            }
+            base += from_lane(end, WAVE - 1);
+            if (!whole) slot += from_lane(slot_end, WAVE - 1);
         }
-        base += from_lane(end, WAVE - 1);
-        slot += from_lane(slot_end, WAVE - 1);
     }
     return it;
 }

@@ -3,6 +3,8 @@
 // and the accumulated weights.
 #include <math.h>
 
+#include <type_traits>
+
 #include "pc_attn.h"
 
 namespace pc {
@@ -556,18 +558,45 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
         for (uint32_t from = (blockIdx.x - tile * row_blocks) * step; from < rows; from += row_blocks * step) {
             const bool there = from + at / teams < rows;
             const uint32_t row = there ? from + at / teams : from;
-            const float2 ml = join_stats(a, it, it.head, it.row_tile, row, lane, LANES);
-            const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
+            const uint32_t part0 = slot_of(a, it, it.head, it.row_tile, 0), apart = it.shape.row_tiles * a.kv.n_kv;
+            // four parts from p on, every teams-th: a part that is not there or saw nothing has the
+            // maximum -inf, and one that saw nothing holds zeros
+            auto parts = [&](uint32_t p, float2 (&y)[4], float4 (&x)[4]) {
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) {
+                    const uint32_t slot = part0 + min(p + u * teams, it.splits - 1) * apart;
+                    const uint64_t i = (uint64_t)min(slot, a.slots - 1) * a.slot_rows + row;
+                    y[u] = a.part_ml[i];
+                    x[u] = *(const float4 *)(a.part + i * D + lane * 4);
+                    if (p + u * teams >= it.splits || slot >= a.slots) y[u].x = MINUS_INF;
+                }
+            };
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (uint32_t p = team; p < it.splits; p += teams) {
-                const uint32_t slot = slot_of(a, it, it.head, it.row_tile, p);
-                if (slot >= a.slots) continue;
-                const uint64_t i = (uint64_t)slot * a.slot_rows + row;
-                const float m = a.part_ml[i].x;
-                if (m == MINUS_INF) continue;
-                const float4 x = *(const float4 *)(a.part + i * D + lane * 4);
-                const float f = exp2_fast(m - ref);
-                sum = make_float4(sum.x + x.x * f, sum.y + x.y * f, sum.z + x.z * f, sum.w + x.w * f);
+            auto add = [&](const float2 (&y)[4], const float4 (&x)[4], float ref) {
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) {
+                    const float f = exp2_fast(y[u].x - ref);
+                    if (y[u].x != MINUS_INF)
+                        sum = make_float4(sum.x + x[u].x * f, sum.y + x[u].y * f, sum.z + x[u].z * f, sum.w + x[u].w * f);
+                }
+            };
+            float2 ml, y[4];
+            float4 x[4];
+            if (teams == 1 && it.splits <= 4) {   // all there is, in one wait
+                parts(0, y, x);
+                ml = make_float2(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), 0.f);
+                const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u)
+                    if (y[u].x != MINUS_INF) ml.y += y[u].y * exp2_fast(y[u].x - ref);
+                add(y, x, ref);
+            } else {
+                ml = join_stats(a, it, it.head, it.row_tile, row, lane, LANES);
+                const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
+                for (uint32_t p = team; p < it.splits; p += 4 * teams) {
+                    parts(p, y, x);
+                    add(y, x, ref);
+                }
             }
             if (teams > 1) {
                 __syncthreads();
@@ -645,7 +674,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
     constexpr int TILE = WEIGHT_ROWS * D * 2;
     __shared__ __attribute__((aligned(16))) char lds[2][TILE];
     __shared__ __attribute__((aligned(16))) float base2[2][WEIGHT_ROWS];
-    __shared__ __attribute__((aligned(16))) int32_t slot_of_row[2][WEIGHT_ROWS];
+    __shared__ __attribute__((aligned(16))) int2 sees[2][WEIGHT_ROWS];   // first and last slot
     const uint32_t tid = threadIdx.x, lane = tid & (WAVE - 1), half = lane / 32, wave = uniform(tid / WAVE), col = lane % 32;
     uint32_t b = blockIdx.x;
     const uint32_t h = b % a.kv.n_kv;
@@ -689,56 +718,59 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
                     else k[n][i] = x;
                 }
             }
+            // the scale's sign, or its zero, goes to the keys; and they are waited for here, else
+            // every pass of the loop would wait for all its loads
+            const uint32_t all = zero ? 0 : ~0u;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    uint4 &x = k[n][i];
+                    x = make_uint4((x.x ^ flip) & all, (x.y ^ flip) & all, (x.z ^ flip) & all, (x.w ^ flip) & all);
+                    __asm__ volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));
+                }
         }
         const uint32_t n_piece = tid % (D / 8);
         const RowAt<D> q_at;
+        const bool no_piece = !FULL && n_piece * 8 >= a.kv.dim;
         uint4 x[PIECES];
         float base = 0.f;
-        int32_t place = 0;
+        int2 see = make_int2(0, -1);
+        // whether a row of the 64 from r0 on is not there or does not see one of keys from .. to
+        auto masks = [&](uint32_t r0, int32_t from, int32_t to) {
+            const int64_t x0 = j0 + a.by_group.div(r0), x1 = j0 + a.by_group.div(min(r0 + WEIGHT_ROWS, r_hi) - 1);
+            return (a.causal && to > x0) || (a.window && (int64_t)from <= x1 - (int64_t)a.window) || to >= (int32_t)k_hi ||
+                   r0 + WEIGHT_ROWS > r_hi;
+        };
+        // rows past the end are the last one's bytes (and masked); nothing here waits for what it loads
         auto load = [&](uint32_t r0) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const uint32_t r = r0 + (tid + 256 * i) / (D / 8);
-                x[i] = make_uint4(0, 0, 0, 0);
-                if (r < r_hi && !zero && (FULL || n_piece * 8 < a.kv.dim)) {
-                    const uint32_t t = a.by_group.div(r), e = h * a.group + (r - t * a.group);
-                    const uint4 y = *(const uint4 *)(a.q + (uint64_t)(q.first + t) * a.q_row + e * a.q_head + n_piece * 16);
-                    x[i] = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
-                }
+                const uint32_t r = min(r0 + (tid + 256 * i) / (D / 8), r_hi - 1);
+                const uint32_t t = a.by_group.div(r), e = h * a.group + (r - t * a.group);
+                x[i] = *(const uint4 *)(a.q + (uint64_t)(q.first + t) * a.q_row + e * a.q_head + (no_piece ? 0 : n_piece * 16));
             }
             if (tid < WEIGHT_ROWS) {
-                base = __builtin_inff();   // exp2(-inf): rows past the end, rows that see nothing
-                place = 0;
-                if (r0 + tid < r_hi) {
-                    const uint32_t t = a.by_group.div(r0 + tid), e = h * a.group + (r0 + tid - t * a.group);
-                    const float y = a.lse2[(uint64_t)(q.first + t) * a.n_heads + e];
-                    base = y == MINUS_INF ? __builtin_inff() : y;
-                    place = (int32_t)(j0 + t);
+                const uint32_t r = min(r0 + tid, r_hi - 1), t = a.by_group.div(r), e = h * a.group + (r - t * a.group);
+                base = a.lse2[(uint64_t)(q.first + t) * a.n_heads + e];
+                if (masks(r0, (int32_t)k0, (int32_t)k0 + WEIGHT_KEYS - 1)) {   // of any wave's keys
+                    seen_by_row(a, q, t, &see.x, &see.y);
+                    if (r0 + tid >= r_hi) see.y = -1;
                 }
             }
         };
         auto store = [&](int buf) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                *(uint4 *)(lds[buf] + piece_at<D>((tid + 256 * i) / (D / 8), n_piece)) = x[i];
+                *(uint4 *)(lds[buf] + piece_at<D>((tid + 256 * i) / (D / 8), n_piece)) = no_piece ? make_uint4(0, 0, 0, 0) : x[i];
             if (tid < WEIGHT_ROWS) {
-                base2[buf][tid] = base;
-                slot_of_row[buf][tid] = place;
+                base2[buf][tid] = base == MINUS_INF ? __builtin_inff() : base;   // a row that sees nothing: exp2(-inf)
+                sees[buf][tid] = see;
             }
         };
-        if (r_lo < r_hi) {
-            load(r_lo);
-            store(0);
-        }
-        __syncthreads();
-        int buf = 0;
         const int32_t w_first = (int32_t)(k0 + wave * 64), w_last = w_first + 63;   // the wave's keys
-        for (uint32_t r0 = r_lo; r0 < r_hi; r0 += WEIGHT_ROWS) {
-            const bool more = r0 + WEIGHT_ROWS < r_hi;
-            if (more) load(r0 + WEIGHT_ROWS);
-            const int64_t x0 = j0 + a.by_group.div(r0), x1 = j0 + a.by_group.div(min(r0 + WEIGHT_ROWS, r_hi) - 1);
-            const bool edge = (a.causal && w_last > x0) || (a.window && (int64_t)w_first <= x1 - (int64_t)a.window) ||
-                              w_last >= (int32_t)k_hi;
+        // 64 rows; `masked` where a row of them does not see a key of the wave's
+        auto add_rows = [&](auto masked, int buf) {
 #pragma unroll
             for (int m = 0; m < WEIGHT_ROWS / 32; ++m) {
                 f32x16 z[2];
@@ -752,19 +784,17 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const float4 l = *(const float4 *)&base2[buf][32 * m + key_of(r, half)];
-                    const int4 place4 = *(const int4 *)&slot_of_row[buf][32 * m + key_of(r, half)];
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         float e[4] = {exp2_fast(fmaf(z[n][r], c, -l.x)), exp2_fast(fmaf(z[n][r + 1], c, -l.y)),
                                       exp2_fast(fmaf(z[n][r + 2], c, -l.z)), exp2_fast(fmaf(z[n][r + 3], c, -l.w))};
-                        if (edge) {
+                        if (masked.value) {
                             const int32_t key = w_first + 32 * n + (int32_t)col;
-                            const int32_t at[4] = {place4.x, place4.y, place4.z, place4.w};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (key >= (int32_t)k_hi || (a.causal && key > at[i]) ||
-                                    (a.window && (int64_t)key <= (int64_t)at[i] - (int64_t)a.window))
-                                    e[i] = 0.f;
+                            for (int i = 0; i < 4; ++i) {
+                                const int2 see = sees[buf][32 * m + key_of(r, half) + i];
+                                if (key >= (int32_t)k_hi || key < see.x || key > see.y) e[i] = 0.f;
+                            }
                         }
                         g[n] += (e[0] + e[1]) + (e[2] + e[3]);
                     }
@@ -772,6 +802,20 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
                 sum[0] += g[0];
                 sum[1] += g[1];
             }
+        };
+        if (r_lo < r_hi) {
+            load(r_lo);
+            store(0);
+        }
+        __syncthreads();
+        int buf = 0;
+        for (uint32_t r0 = r_lo; r0 < r_hi; r0 += WEIGHT_ROWS) {
+            const bool more = r0 + WEIGHT_ROWS < r_hi;
+            if (more) load(r0 + WEIGHT_ROWS);
+            if (masks(r0, w_first, w_last))
+                add_rows(std::true_type{}, buf);
+            else
+                add_rows(std::false_type{}, buf);
             if (more) store(buf ^ 1);
             __syncthreads();
             buf ^= 1;
@@ -809,13 +853,18 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(AttnArgs a, uint32_t ke
 // ---------------------------------------------------------------------- host
 
 constexpr uint32_t ROWS_MOST = 32;           // rows of the path for few rows
-constexpr uint32_t ROWS_ITEMS = 1024, CHUNK_ITEMS = 512;
+constexpr uint32_t ROWS_ITEMS = 1024;
+// Two workgroups of chunk_kernel fit a compute unit: 512 items are one round of them.  Of
+// a few sequences they come out alike; of several, uneven lengths leave gaps that
+// smaller items fill (12 ragged chunks: @R@), which costs a join where there
+// was none (one chunk of 2,048 over 32,768: 18 us of 1,160).
+constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
 constexpr uint32_t WEIGHT_ITEMS = 1024;
 
 struct AttnPlan {
     bool few;
-    uint32_t dim, slots, slot_rows, weight_parts, key_blocks;
+    uint32_t dim, items, slots, slot_rows, weight_parts, key_blocks;
     uint64_t score_stride;
 };
 static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim) {
@@ -824,7 +873,8 @@ static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint
     p.few = (uint64_t)max_q * group <= ROWS_MOST;
     p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
     // an item that is a part has more than half an item's tiles: at most two per item wanted
-    p.slots = 2 * (p.few ? ROWS_ITEMS : CHUNK_ITEMS);
+    p.items = p.few ? ROWS_ITEMS : n_seqs < RAGGED_SEQS ? CHUNK_ITEMS : CHUNK_ITEMS_RAGGED;
+    p.slots = 2 * p.items;
     p.slot_rows = p.few ? (max_q ? max_q : 1) * group : CHUNK_ROWS;
     p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
     p.key_blocks = (uint32_t)(((uint64_t)max_kv + WEIGHT_KEYS - 1) / WEIGHT_KEYS);
@@ -869,7 +919,7 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, 
     // a tile (most of them find whole results and end)
     constexpr uint32_t ALL = 256 / (D / 4);
     uint32_t teams = ALL;
-    while (teams > 1 && tiles * p.slot_rows * teams / ALL > 4096) teams /= 2;
+    while (teams > 1 && tiles * p.slot_rows * teams / ALL > 1024) teams /= 2;
     uint32_t row_blocks = (p.slot_rows * teams + ALL - 1) / ALL;
     while (row_blocks > 1 && tiles * row_blocks > 2048) row_blocks = (row_blocks + 1) / 2;
     const uint32_t key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
@@ -959,7 +1009,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.causal = flags & PC_ATTN_CAUSAL;
     a.window = window;
     a.by_16 = a.kv.page % 16 == 0 && a.kv.st < (1u << 24);
-    a.target = p.few ? ROWS_ITEMS : CHUNK_ITEMS;
+    a.target = p.items;
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);

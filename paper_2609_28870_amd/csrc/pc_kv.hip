@@ -37,6 +37,9 @@ pc_status kv_view(const pc_kv_cache *c, KvView *v) {
 // A copy with an index: bound by memory, or for a few tokens by the one launch
 // and its chain of loads (the row's sequence, its length, its page).
 
+constexpr uint32_t APPEND_MANY = 8192;   // rows: as many as the chip holds waves
+constexpr uint32_t APPEND_ROWS = 4;      // of a wave, then
+
 struct AppendArgs {
     KvView kv;
     const uint32_t *table, *kv_len, *q_off;
@@ -46,6 +49,7 @@ struct AppendArgs {
     uint64_t k_row, k_head, v_row, v_head;
     int32_t *status;
     FastDiv by_head;     // 16-byte pieces of one head's cache entry
+    FastDiv by_token;    // and of a token's
     uint32_t pieces;     // of one token
 };
 
@@ -107,14 +111,15 @@ __device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b, float scale)
     return (uint32_t)w;
 }
 
-// MODE 0: the types agree; 1, 2: an 8-bit cache from bf16, f16
+// Few rows: a wave each, so that the row's chain of loads is all there is and its
+// addresses are scalar.  MODE 0: the types agree; 1, 2: an 8-bit cache from bf16, f16.
+// 255 rows: 3.6 us; the kernel below takes 8.5 with one row a wave.
 template <int MODE>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256) void append_few_kernel(AppendArgs a) {
     if (blockIdx.x == 0) {
         append_status(a);
         return;
     }
-    // a wave per token
     const int lane = threadIdx.x & (WAVE - 1);
     const uint32_t t = (blockIdx.x - 1) * (256 / WAVE) + threadIdx.x / WAVE;
     if (t >= a.n_rows) return;
@@ -148,6 +153,97 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     }
 }
 
+// sequence of chunk row t, by a whole wave: the first that ends past it (or the last one)
+__device__ __forceinline__ uint32_t wave_seq_of(const uint32_t *__restrict__ q_off, uint32_t n_seqs, uint32_t t) {
+    const uint32_t lane = threadIdx.x & (WAVE - 1);
+    uint32_t lo = 0, n = n_seqs;   // one of lo .. lo + n - 1
+    while (n > 1) {
+        const uint32_t step = (n + WAVE - 1) / WAVE;
+        const bool in = lane * step < n;
+        const uint32_t end = in ? q_off[lo + min((lane + 1) * step, n)] : 0;
+        const uint32_t past = min((uint32_t)__popcll(ballot(in && end <= t)) * step, n - 1);
+        lo += past;
+        n = min(step, n - past);
+        if (step == 1) break;
+    }
+    return lo;
+}
+
+// Many rows: four to a wave, whose lanes take the 16-byte pieces of their cache
+// entries, so that the chain's wait is shared and no lane idles.
+// 21,100 rows of bf16 into an 8-bit cache (4 heads of 128, 65 MB): 18 us, 3.6 TB/s (a
+// row a wave: 24.5).
+template <int MODE>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+    constexpr int TOKENS = APPEND_ROWS;
+    if (blockIdx.x == 0) {
+        append_status(a);
+        return;
+    }
+    const uint32_t lane = threadIdx.x & (WAVE - 1);
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / WAVE));
+    const uint32_t t0 = ((blockIdx.x - 1) * (256 / WAVE) + wave) * TOKENS;
+    if (t0 >= a.n_rows) return;
+    const uint32_t s0 = wave_seq_of(a.q_off, a.n_seqs, t0), rows = min((uint32_t)TOKENS, a.n_rows - t0);
+    constexpr int AT_ONCE = MODE ? 1 : 2, IN = MODE ? 2 : 1;   // 64 bytes a lane
+    for (uint32_t p0 = lane; p0 < rows * a.pieces; p0 += AT_ONCE * WAVE) {
+        uint4 x[AT_ONCE][IN], y[AT_ONCE][IN];
+        uint64_t to[AT_ONCE];
+        uint32_t head[AT_ONCE];
+        bool there[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint32_t p = p0 + u * WAVE, i = min(a.by_token.div(p), rows - 1), t = t0 + i;
+            const uint32_t of = p - i * a.pieces, h = a.by_head.div(of), c = of - h * a.by_head.d;
+            uint32_t s = s0;
+            while (s + 1 < a.n_seqs && a.q_off[s + 1] <= t) ++s;
+            bool bad;
+            const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
+            const int64_t slot = (int64_t)q.len - q.rows + (t - q.first);
+            there[u] = p < rows * a.pieces && t >= q.first && t - q.first < q.rows && slot >= 0;
+            if (!there[u]) continue;
+            const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;
+            const uint32_t page = a.table[(uint64_t)s * a.table_stride + at];
+            there[u] = page < a.kv.n_pages;
+            to[u] = page * a.kv.sp + off * a.kv.st + h * a.kv.sh + c * 16;
+            head[u] = h;
+            const uint4 *k = (const uint4 *)(a.k + t * a.k_row + h * a.k_head) + c * IN;
+            const uint4 *v = (const uint4 *)(a.v + t * a.v_row + h * a.v_head) + c * IN;
+#pragma unroll
+            for (int j = 0; j < IN; ++j) {
+                x[u][j] = k[j];
+                y[u][j] = v[j];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (!there[u]) continue;
+            if (MODE) {
+                constexpr int HI = IN - 1;
+                const float ks = a.kv.k_scale[head[u]], vs = a.kv.v_scale[head[u]];
+                const uint4 x0 = x[u][0], x1 = x[u][HI], y0 = y[u][0], y1 = y[u][HI];
+                *(uint4 *)(a.kv.k + to[u]) = make_uint4(to_e4m3<MODE == 1>(x0.x, x0.y, ks), to_e4m3<MODE == 1>(x0.z, x0.w, ks),
+                                                        to_e4m3<MODE == 1>(x1.x, x1.y, ks), to_e4m3<MODE == 1>(x1.z, x1.w, ks));
+                *(uint4 *)(a.kv.v + to[u]) = make_uint4(to_e4m3<MODE == 1>(y0.x, y0.y, vs), to_e4m3<MODE == 1>(y0.z, y0.w, vs),
+                                                        to_e4m3<MODE == 1>(y1.x, y1.y, vs), to_e4m3<MODE == 1>(y1.z, y1.w, vs));
+            } else {
+                *(uint4 *)(a.kv.k + to[u]) = x[u][0];
+                *(uint4 *)(a.kv.v + to[u]) = y[u][0];
+            }
+        }
+    }
+}
+
+template <int MODE>
+static pc_status append_run(const AppendArgs &a, hipStream_t st) {
+    const bool many = a.n_rows >= APPEND_MANY;
+    const uint32_t per = (many ? APPEND_ROWS : 1) * (256 / WAVE);
+    const dim3 grid(1 + (a.n_rows + per - 1) / per);
+    if (many) PC_LAUNCH(K_KV_APPEND, append_kernel<MODE>, grid, dim3(256), 0, st, a);
+    else PC_LAUNCH(K_KV_APPEND, append_few_kernel<MODE>, grid, dim3(256), 0, st, a);
+    return PC_OK;
+}
+
 // -------------------------------------------------------------------- evict
 
 struct EvictArgs {
@@ -169,14 +265,36 @@ __device__ __forceinline__ uint32_t order_of(float f) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-constexpr int SELECT_THREADS = 1024;
+constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / WAVE;
+constexpr uint32_t DIGITS = 2048;   // bins of a histogram
 
-// One workgroup per (sequence, head): the need-th largest key by four digits of
-// eight bits (a histogram each), then the kept slots in order.
+// Adds this lane's digit to the histogram.  Weights are heavy-tailed and often tied, so
+// most lanes of a wave meet in one bin, where atomics would follow each other: the
+// first lane adds for all that have its digit, the others for themselves.
+__device__ __forceinline__ void count_digit(uint32_t *hist, bool in, uint32_t digit) {
+    const uint64_t all = ballot(in);
+    if (!all) return;
+    const uint32_t lead = (uint32_t)__ffsll((unsigned long long)all) - 1;
+    const bool same = in & (digit == (uint32_t)__builtin_amdgcn_readlane((int)digit, (int)lead));
+    const uint32_t n = (uint32_t)__popcll(ballot(same)), lane = threadIdx.x & (WAVE - 1);
+    if (in & (!same | (lane == lead))) atomicAdd(&hist[digit], same ? n : 1u);
+}
+
+// One workgroup per (sequence, head): the need-th largest weight by digits of 11, 11
+// and 10 bits (a histogram each), then the kept slots in order.  A wave has `steps`
+// times 64 consecutive slots, a lane every 64th.  Rows of up to 8192 slots stay in
+// registers (KEYS = 8 a thread); longer ones are read again for each pass from the
+// cache, eight slots of a thread ahead of the eight it works on (KEYS = 0).  Key 0 is no
+// weight's: slots past the end and the last ones, which stay whatever their weights.
+// Bound by one compute unit's instructions on the longest row.  (65536 slots in
+// registers took as long as reading them again and again: the loops
+// are then unrolled into 40 KB of code, which is fetched once a launch.)
+template <int KEYS>
 __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[256], tmp[2 * SELECT_THREADS / WAVE];
+    __shared__ uint32_t hist[DIGITS], tmp[SELECT_WAVES], above_of[SELECT_WAVES], ties_of[SELECT_WAVES];
     __shared__ uint32_t pick, left;
     const uint32_t s = blockIdx.x / a.kv.n_kv, h = blockIdx.x - s * a.kv.n_kv, tid = threadIdx.x;
+    const uint32_t lane = tid & (WAVE - 1), wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid / WAVE));
     if (blockIdx.x == 0) {   // the call's status word; the pages are the move's to check
         bool bad = false;
         for (uint32_t i = tid; i < a.n_seqs; i += SELECT_THREADS) bad |= a.kv_len[i] > a.max_kv;
@@ -190,59 +308,115 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
     uint32_t *kept = a.kept + row * a.budget;
     float *wout = a.weight_out ? a.weight_out + row * a.budget : nullptr;
     if (h == 0 && tid == 0) a.new_len[s] = n;
-    uint32_t floor_key = 0, equal = need;   // keys above floor_key stay, and `equal` of those at it
-    if (need < cand && need > 0) {
-        uint32_t known = 0, mask = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
+    // the places that need no choice: the last slots, and none
+    for (uint32_t r = need + tid; r < a.budget; r += SELECT_THREADS) {
+        const uint32_t j = cand + (r - need);
+        kept[r] = r < n ? j : NONE;
+        if (wout) wout[r] = r < n ? w[j] : 0.f;
+    }
+    if (!need) return;
+    const uint32_t steps = (cand + SELECT_WAVES * 8 * WAVE - 1) / (SELECT_WAVES * 8 * WAVE) * 8;
+    const uint32_t j0 = wave * steps * WAVE + lane;
+    uint32_t keys[8];
+    auto load = [&](uint32_t step, uint32_t *key) {   // eight at once
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) key[i] = __float_as_uint(w[min(j0 + (step + i) * WAVE, cand - 1)]);
+    };
+    auto order = [&](uint32_t step, uint32_t *key) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) key[i] = j0 + (step + i) * WAVE < cand ? order_of(__uint_as_float(key[i])) : 0;
+    };
+    auto visit = [&](auto body) {
+        if (KEYS) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) body(i, keys[i]);
+            return;
+        }
+        uint32_t next[8];
+        load(0, next);
+#pragma unroll 1
+        for (uint32_t g = 0; g < steps; g += 8) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) keys[i] = next[i];
+            load(g + 8, next);   // past the end: the last slot
+            order(g, keys);
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) body(g + i, keys[i]);
+        }
+    };
+    if (KEYS) {
+        load(0, keys);
+        order(0, keys);
+    }
+    uint32_t floor_key = 0, equal = 0;   // keys above floor_key stay, and `equal` of those at it
+    if (need < cand) {
+        equal = need;
+#pragma unroll 1   // small code: of a few-microsecond call much is the first fetch of its instructions
+        for (int digit = 0; digit < 3; ++digit) {
+            const uint32_t shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
+            const uint32_t mask = digit == 0 ? 0 : digit == 1 ? ~0u << 21 : ~0u << 10;
+            hist[tid] = hist[tid + SELECT_THREADS] = 0;
             __syncthreads();
-            for (uint32_t j = tid; j < cand; j += SELECT_THREADS) {
-                const uint32_t key = order_of(w[j]);
-                if ((key & mask) == known) atomicAdd(&hist[key >> shift & 255], 1u);
-            }
+            visit([&](uint32_t, uint32_t key) {
+                count_digit(hist, (key != 0) & ((key & mask) == floor_key), key >> shift & (bins - 1));
+            });
             __syncthreads();
+            // the largest digits first, two a thread
+            const uint32_t hi = hist[DIGITS - 1 - 2 * tid], lo = hist[DIGITS - 2 - 2 * tid];
             uint32_t total;
-            const uint32_t c = tid < 256 ? hist[255 - tid] : 0;
-            const uint32_t above = block_excl_scan(c, tmp, &total);   // digits larger than 255 - tid
-            if (tid < 256 && above < equal && above + c >= equal) {
-                pick = 255 - tid;
-                left = equal - above;
+            const uint32_t above = block_excl_scan(hi + lo, tmp, &total);
+            if (above < equal && above + hi + lo >= equal) {
+                const bool first = above + hi >= equal;
+                pick = DIGITS - 1 - 2 * tid - (first ? 0 : 1);
+                left = equal - above - (first ? 0 : hi);
             }
             __syncthreads();
-            known |= pick << shift;
-            mask |= 255u << shift;
+            floor_key |= pick << shift;
             equal = left;
-            __syncthreads();
         }
-        floor_key = known;
     }
-    const bool all = need == cand;
-    uint32_t placed = 0, ties = 0;
-    for (uint32_t j0 = 0; j0 < len; j0 += SELECT_THREADS) {
-        const uint32_t j = j0 + tid;
-        const float x = j < len ? w[j] : 0.f;
-        const uint32_t key = order_of(x);
-        const bool in = j < cand && need > 0;
-        const bool tie = in && !all && key == floor_key;
-        uint32_t t_all, k_all;
-        const uint32_t t = ties + block_excl_scan(tie, tmp, &t_all);
-        const bool keep = (j >= cand && j < len) || (in && (all || key > floor_key || (tie && t < equal)));
-        const uint32_t at = placed + block_excl_scan(keep, tmp, &k_all);
-        if (keep) {
-            kept[at] = j;
-            if (wout) wout[at] = x;
-        }
-        ties += t_all;
-        placed += k_all;
+    // how many of each wave's slots stay, then their places
+    uint32_t above = 0, ties = 0;
+    visit([&](uint32_t, uint32_t key) {
+        above += (uint32_t)__popcll(ballot(key > floor_key));
+        ties += (uint32_t)__popcll(ballot((key != 0) & (key == floor_key)));
+    });
+    if (lane == 0) {
+        above_of[wave] = above;
+        ties_of[wave] = ties;
     }
-    for (uint32_t r = n + tid; r < a.budget; r += SELECT_THREADS) {
-        kept[r] = NONE;
-        if (wout) wout[r] = 0.f;
+    __syncthreads();
+    uint32_t at = 0, quota = equal;   // quota: ties left to this wave and those behind it
+    for (uint32_t i = 0; i < wave; ++i) {
+        const uint32_t t = min(ties_of[i], quota);
+        at += above_of[i] + t;
+        quota -= t;
+    }
+    visit([&](uint32_t step, uint32_t key) {
+        const bool tie = (key != 0) & (key == floor_key);
+        const uint64_t tied = ballot(tie);
+        const bool keep = (key > floor_key) | (tie & (mbcnt_acc(tied, 0) < quota));
+        quota -= min(quota, (uint32_t)__popcll(tied));
+        const uint64_t all = ballot(keep);
+        if (keep) kept[at + mbcnt_acc(all, 0)] = j0 + step * WAVE;
+        at += (uint32_t)__popcll(all);
+    });
+    if (!wout) return;
+    __syncthreads();
+    for (uint32_t r0 = tid; r0 < need; r0 += 4 * SELECT_THREADS) {
+        float x[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) x[i] = w[kept[min(r0 + i * SELECT_THREADS, need - 1)]];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (r0 + i * SELECT_THREADS < need) wout[r0 + i * SELECT_THREADS] = x[i];
     }
 }
 
 constexpr uint32_t MOVE_SLOTS = 64;   // slots of one (sequence, head) per workgroup
 
+// Keys and values of the kept slots, each a run of 16-byte pieces: bound by memory.  (Pieces
+// looked up and loaded four at a time took 100 us for what this does in 84, and 9 for 4.)
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t groups) {
     const uint32_t row = blockIdx.x / groups, r0 = (blockIdx.x - row * groups) * MOVE_SLOTS;
     const uint32_t s = row / a.kv.n_kv, h = row - s * a.kv.n_kv;
@@ -308,11 +482,9 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     a.status = (int32_t *)ws;
     a.by_head = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
     a.pieces = a.by_head.d * a.kv.n_kv;
-    const unsigned grid = 1 + (n_rows + 3) / 4;
-    if (cache->dtype != PC_FP8_E4M3) PC_LAUNCH(K_KV_APPEND, append_kernel<0>, dim3(grid), dim3(256), 0, st, a);
-    else if (dtype == PC_BF16) PC_LAUNCH(K_KV_APPEND, append_kernel<1>, dim3(grid), dim3(256), 0, st, a);
-    else PC_LAUNCH(K_KV_APPEND, append_kernel<2>, dim3(grid), dim3(256), 0, st, a);
-    return PC_OK;
+    a.by_token = fast_div(a.pieces);
+    if (cache->dtype != PC_FP8_E4M3) return append_run<0>(a, st);
+    return dtype == PC_BF16 ? append_run<1>(a, st) : append_run<2>(a, st);
 }
 
 size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv) {
@@ -359,7 +531,8 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     const unsigned rows = n_seqs * a.kv.n_kv;
     const uint32_t groups = (budget < max_kv ? budget : max_kv) / MOVE_SLOTS + 1;
     if (dst_table && (uint64_t)rows * groups > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
-    PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
+    if (max_kv <= 8u * SELECT_THREADS) PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel<8>, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
+    else PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel<0>, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
     if (dst_table) PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel, dim3(rows * groups), dim3(256), 0, st, a, groups);
     return PC_OK;
 }

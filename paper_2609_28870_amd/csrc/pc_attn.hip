@@ -856,11 +856,11 @@ constexpr uint32_t ROWS_MOST = 32;           // rows of the path for few rows
 constexpr uint32_t ROWS_ITEMS = 1024;
 // Two workgroups of chunk_kernel fit a compute unit: 512 items are one round of them.  Of
 // a few sequences they come out alike; of several, uneven lengths leave gaps that
-// smaller items fill (12 ragged chunks: @R@), which costs a join where there
+// smaller items fill (12 ragged chunks: 227 to 197 us), which costs a join where there
 // was none (one chunk of 2,048 over 32,768: 18 us of 1,160).
 constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
-constexpr uint32_t WEIGHT_ITEMS = 1024;
+constexpr uint32_t WEIGHT_ITEMS = 4096;
 
 struct AttnPlan {
     bool few;

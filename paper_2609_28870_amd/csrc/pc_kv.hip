@@ -280,137 +280,234 @@ __device__ __forceinline__ void count_digit(uint32_t *hist, bool in, uint32_t di
     if (in & (!same | (lane == lead))) atomicAdd(&hist[digit], same ? n : 1u);
 }
 
-// One workgroup per (sequence, head): the need-th largest weight by digits of 11, 11
-// and 10 bits (a histogram each), then the kept slots in order.  A wave has `steps`
-// times 64 consecutive slots, a lane every 64th.  Rows of up to 8192 slots stay in
-// registers (KEYS = 8 a thread); longer ones are read again for each pass from the
-// cache, eight slots of a thread ahead of the eight it works on (KEYS = 0).  Key 0 is no
-// weight's: slots past the end and the last ones, which stay whatever their weights.
-// Bound by one compute unit's instructions on the longest row.  (65536 slots in
-// registers took as long as reading them again and again: the loops
-// are then unrolled into 40 KB of code, which is fetched once a launch.)
-template <int KEYS>
-__global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[DIGITS], tmp[SELECT_WAVES], above_of[SELECT_WAVES], ties_of[SELECT_WAVES];
+// What one (sequence, head) keeps: `need` of the first `cand` slots, and all behind them.
+struct EvictRow {
+    uint32_t s, h, cand, need, n;
+    const float *w;
+    uint32_t *kept;
+    float *wout;   // or nullptr
+};
+__device__ __forceinline__ EvictRow evict_row(const EvictArgs &a, uint32_t row) {
+    EvictRow r;
+    r.s = row / a.kv.n_kv;
+    r.h = row - r.s * a.kv.n_kv;
+    const uint32_t len = min(a.kv_len[r.s], a.max_kv);
+    r.n = min(len, a.budget);
+    const uint32_t late = min(a.recent, r.n);
+    r.cand = len - late;
+    r.need = r.n - late;
+    r.w = a.weight + (uint64_t)row * a.weight_stride;
+    r.kept = a.kept + (uint64_t)row * a.budget;
+    r.wout = a.weight_out ? a.weight_out + (uint64_t)row * a.budget : nullptr;
+    return r;
+}
+// the call's status word (the pages are the move's to check), by one workgroup
+__device__ __forceinline__ void evict_status(const EvictArgs &a) {
+    bool bad = false;
+    for (uint32_t i = threadIdx.x; i < a.n_seqs; i += SELECT_THREADS) bad |= a.kv_len[i] > a.max_kv;
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *a.status = any ? DEV_ERR_BAD_LAYOUT : 0;
+}
+// the places that need no choice: the last slots, and none behind them (part of `parts`)
+__device__ __forceinline__ void place_rest(const EvictArgs &a, const EvictRow &e, uint32_t part, uint32_t parts) {
+    if (e.h == 0 && part == 0 && threadIdx.x == 0) a.new_len[e.s] = e.n;
+    for (uint32_t r = e.need + part * SELECT_THREADS + threadIdx.x; r < a.budget; r += parts * SELECT_THREADS) {
+        const uint32_t j = e.cand + (r - e.need);
+        e.kept[r] = r < e.n ? j : NONE;
+        if (e.wout) e.wout[r] = r < e.n ? e.w[j] : 0.f;
+    }
+}
+// This thread's keys: slots j0 + 64 i.  Key 0 is no weight's: slots past the candidates.
+template <int N>
+__device__ __forceinline__ void load_keys(const EvictRow &e, uint32_t j0, uint32_t (&key)[N]) {
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = e.w[min(j0 + i * WAVE, e.cand - 1)];
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = j0 + i * WAVE < e.cand ? order_of(x[i]) : 0;
+}
+// digit number 0, 1 or 2 of a key, from the top
+__device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+template <int N>
+__device__ __forceinline__ void count_digits(uint32_t *hist, const uint32_t (&key)[N], int digit, uint32_t known) {
+    const uint32_t shift = digit_shift(digit), bins = digit == 2 ? 1024 : 2048;
+    const uint32_t mask = digit == 0 ? 0 : digit == 1 ? ~0u << 21 : ~0u << 10;
+    hist[threadIdx.x] = hist[threadIdx.x + SELECT_THREADS] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) count_digit(hist, (key[i] != 0) & ((key[i] & mask) == known), key[i] >> shift & (bins - 1));
+    __syncthreads();
+}
+// The digit of the `equal`-th largest key, from the counts of two digits a thread (the
+// largest digits first); *equal becomes its place among the keys of that digit.
+__device__ __forceinline__ uint32_t pick_digit(uint32_t hi, uint32_t lo, uint32_t *equal, uint32_t *tmp) {
     __shared__ uint32_t pick, left;
-    const uint32_t s = blockIdx.x / a.kv.n_kv, h = blockIdx.x - s * a.kv.n_kv, tid = threadIdx.x;
-    const uint32_t lane = tid & (WAVE - 1), wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid / WAVE));
-    if (blockIdx.x == 0) {   // the call's status word; the pages are the move's to check
-        bool bad = false;
-        for (uint32_t i = tid; i < a.n_seqs; i += SELECT_THREADS) bad |= a.kv_len[i] > a.max_kv;
-        const int any = __syncthreads_or(bad);
-        if (tid == 0) *a.status = any ? DEV_ERR_BAD_LAYOUT : 0;
+    uint32_t total;
+    const uint32_t above = block_excl_scan(hi + lo, tmp, &total);
+    if (above < *equal && above + hi + lo >= *equal) {
+        const bool first = above + hi >= *equal;
+        pick = DIGITS - 1 - 2 * threadIdx.x - (first ? 0 : 1);
+        left = *equal - above - (first ? 0 : hi);
     }
-    const uint32_t len = min(a.kv_len[s], a.max_kv), n = min(len, a.budget), late = min(a.recent, n);
-    const uint32_t cand = len - late, need = n - late;   // need of the first cand slots stay
-    const uint64_t row = (uint64_t)s * a.kv.n_kv + h;
-    const float *w = a.weight + row * a.weight_stride;
-    uint32_t *kept = a.kept + row * a.budget;
-    float *wout = a.weight_out ? a.weight_out + row * a.budget : nullptr;
-    if (h == 0 && tid == 0) a.new_len[s] = n;
-    // the places that need no choice: the last slots, and none
-    for (uint32_t r = need + tid; r < a.budget; r += SELECT_THREADS) {
-        const uint32_t j = cand + (r - need);
-        kept[r] = r < n ? j : NONE;
-        if (wout) wout[r] = r < n ? w[j] : 0.f;
-    }
-    if (!need) return;
-    const uint32_t steps = (cand + SELECT_WAVES * 8 * WAVE - 1) / (SELECT_WAVES * 8 * WAVE) * 8;
-    const uint32_t j0 = wave * steps * WAVE + lane;
-    uint32_t keys[8];
-    auto load = [&](uint32_t step, uint32_t *key) {   // eight at once
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) key[i] = __float_as_uint(w[min(j0 + (step + i) * WAVE, cand - 1)]);
-    };
-    auto order = [&](uint32_t step, uint32_t *key) {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) key[i] = j0 + (step + i) * WAVE < cand ? order_of(__uint_as_float(key[i])) : 0;
-    };
-    auto visit = [&](auto body) {
-        if (KEYS) {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) body(i, keys[i]);
-            return;
-        }
-        uint32_t next[8];
-        load(0, next);
-#pragma unroll 1
-        for (uint32_t g = 0; g < steps; g += 8) {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) keys[i] = next[i];
-            load(g + 8, next);   // past the end: the last slot
-            order(g, keys);
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) body(g + i, keys[i]);
-        }
-    };
-    if (KEYS) {
-        load(0, keys);
-        order(0, keys);
-    }
-    uint32_t floor_key = 0, equal = 0;   // keys above floor_key stay, and `equal` of those at it
-    if (need < cand) {
-        equal = need;
-#pragma unroll 1   // small code: of a few-microsecond call much is the first fetch of its instructions
-        for (int digit = 0; digit < 3; ++digit) {
-            const uint32_t shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
-            const uint32_t mask = digit == 0 ? 0 : digit == 1 ? ~0u << 21 : ~0u << 10;
-            hist[tid] = hist[tid + SELECT_THREADS] = 0;
-            __syncthreads();
-            visit([&](uint32_t, uint32_t key) {
-                count_digit(hist, (key != 0) & ((key & mask) == floor_key), key >> shift & (bins - 1));
-            });
-            __syncthreads();
-            // the largest digits first, two a thread
-            const uint32_t hi = hist[DIGITS - 1 - 2 * tid], lo = hist[DIGITS - 2 - 2 * tid];
-            uint32_t total;
-            const uint32_t above = block_excl_scan(hi + lo, tmp, &total);
-            if (above < equal && above + hi + lo >= equal) {
-                const bool first = above + hi >= equal;
-                pick = DIGITS - 1 - 2 * tid - (first ? 0 : 1);
-                left = equal - above - (first ? 0 : hi);
-            }
-            __syncthreads();
-            floor_key |= pick << shift;
-            equal = left;
-        }
-    }
-    // how many of each wave's slots stay, then their places
+    __syncthreads();
+    *equal = left;
+    return pick;
+}
+// The kept ones of a workgroup's keys to their places, from `at` on: those above floor_key, and
+// `quota` at most of those equal to it.  A wave's slots are consecutive, and so are the waves'.
+template <int N>
+__device__ __forceinline__ void place_kept(const EvictRow &e, const uint32_t (&key)[N], uint32_t j0, uint32_t floor_key,
+                                           uint32_t at, uint32_t quota) {
+    __shared__ uint32_t above_of[SELECT_WAVES], ties_of[SELECT_WAVES];
+    const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid / WAVE));
     uint32_t above = 0, ties = 0;
-    visit([&](uint32_t, uint32_t key) {
-        above += (uint32_t)__popcll(ballot(key > floor_key));
-        ties += (uint32_t)__popcll(ballot((key != 0) & (key == floor_key)));
-    });
-    if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        above += (uint32_t)__popcll(ballot(key[i] > floor_key));
+        ties += (uint32_t)__popcll(ballot((key[i] != 0) & (key[i] == floor_key)));
+    }
+    if (tid % WAVE == 0) {
         above_of[wave] = above;
         ties_of[wave] = ties;
     }
     __syncthreads();
-    uint32_t at = 0, quota = equal;   // quota: ties left to this wave and those behind it
-    for (uint32_t i = 0; i < wave; ++i) {
-        const uint32_t t = min(ties_of[i], quota);
-        at += above_of[i] + t;
-        quota -= t;
+    const uint32_t first = at;
+    uint32_t end = at, left = quota;
+    for (uint32_t i = 0; i < (uint32_t)SELECT_WAVES; ++i) {
+        if (i == wave) {
+            at = end;
+            quota = left;
+        }
+        const uint32_t t = min(ties_of[i], left);
+        end += above_of[i] + t;
+        left -= t;
     }
-    visit([&](uint32_t step, uint32_t key) {
-        const bool tie = (key != 0) & (key == floor_key);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool tie = (key[i] != 0) & (key[i] == floor_key);
         const uint64_t tied = ballot(tie);
-        const bool keep = (key > floor_key) | (tie & (mbcnt_acc(tied, 0) < quota));
+        const bool keep = (key[i] > floor_key) | (tie & (mbcnt_acc(tied, 0) < quota));
         quota -= min(quota, (uint32_t)__popcll(tied));
         const uint64_t all = ballot(keep);
-        if (keep) kept[at + mbcnt_acc(all, 0)] = j0 + step * WAVE;
+        if (keep) e.kept[at + mbcnt_acc(all, 0)] = j0 + i * WAVE;
         at += (uint32_t)__popcll(all);
-    });
-    if (!wout) return;
+    }
+    if (!e.wout) return;
     __syncthreads();
-    for (uint32_t r0 = tid; r0 < need; r0 += 4 * SELECT_THREADS) {
+    for (uint32_t r0 = first + tid; r0 < end; r0 += 4 * SELECT_THREADS) {
         float x[4];
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) x[i] = w[kept[min(r0 + i * SELECT_THREADS, need - 1)]];
+        for (uint32_t i = 0; i < 4; ++i) x[i] = e.w[e.kept[min(r0 + i * SELECT_THREADS, end - 1)]];
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
-            if (r0 + i * SELECT_THREADS < need) wout[r0 + i * SELECT_THREADS] = x[i];
+            if (r0 + i * SELECT_THREADS < end) e.wout[r0 + i * SELECT_THREADS] = x[i];
     }
+}
+
+// The selection: the need-th largest weight by digits of 11, 11 and 10 bits (a histogram
+// each), then the kept slots in order.  Bound by one compute unit's instructions, about
+// 25 a slot and pass, and by a few waits.
+
+// Rows of up to 8192 slots: one workgroup per (sequence, head), the keys in registers.
+// 4 rows of 4,099 slots: 10 us (reading them again for each pass of 8-bit digits: 17.5).
+constexpr int ROW_KEYS = 8;
+__global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs a) {
+    __shared__ uint32_t hist[DIGITS], tmp[SELECT_WAVES];
+    if (blockIdx.x == 0) evict_status(a);
+    const EvictRow e = evict_row(a, blockIdx.x);
+    place_rest(a, e, 0, 1);
+    if (!e.need) return;
+    const uint32_t tid = threadIdx.x, j0 = tid / WAVE * (ROW_KEYS * WAVE) + tid % WAVE;
+    uint32_t key[ROW_KEYS];
+    load_keys(e, j0, key);
+    uint32_t floor_key = 0, equal = 0;   // keys above floor_key stay, and `equal` of those at it
+    if (e.need < e.cand) {
+        equal = e.need;
+#pragma unroll 1   // small code: of a few-microsecond call much is the first fetch of its instructions
+        for (int digit = 0; digit < 3; ++digit) {
+            count_digits(hist, key, digit, floor_key);
+            floor_key |= pick_digit(hist[DIGITS - 1 - 2 * tid], hist[DIGITS - 2 - 2 * tid], &equal, tmp) << digit_shift(digit);
+        }
+    }
+    place_kept(e, key, j0, floor_key, 0, equal);
+}
+
+// Longer rows: a workgroup per segment of 16384 slots, and a launch per digit, since
+// the segments have to meet: each phase adds up its row's histograms of the digit before
+// and counts the next; the last one places.  What a segment needs to know of those
+// before it (the keys above the digit) follows from their histograms.
+// 16 sequences of 4 heads, 303k slots, the longest 65,536: 32 us in four launches (one workgroup a row: 60, keys
+// in registers, or 71).
+constexpr int SEGMENT_KEYS = 16;
+constexpr uint32_t SEGMENT = SEGMENT_KEYS * SELECT_THREADS;
+struct EvictSplit {
+    uint32_t segments;   // of a row
+    uint64_t all;        // of the call
+    uint32_t *hist;      // [2][row][segment][digit], used in turn
+    uint32_t *above;     // [2][row][segment] keys above the first and second digit
+    uint2 *state;        // [2][row] digits known, place among the keys that have them
+};
+template <int PHASE>
+__global__ __launch_bounds__(SELECT_THREADS) void evict_split_kernel(EvictArgs a, EvictSplit b) {
+    __shared__ uint32_t hist[DIGITS], tmp[SELECT_WAVES];
+    __shared__ uint32_t tied;
+    const uint32_t row = blockIdx.x / b.segments, segment = blockIdx.x - row * b.segments, tid = threadIdx.x;
+    if (PHASE == 0 && blockIdx.x == 0) evict_status(a);
+    const EvictRow e = evict_row(a, row);
+    if (PHASE == 3) place_rest(a, e, segment, b.segments);
+    if (!e.need || segment * SEGMENT >= e.cand) return;
+    const bool all = e.need == e.cand;
+    if (PHASE < 3 && all) return;
+    const uint32_t j0 = segment * SEGMENT + tid / WAVE * (SEGMENT_KEYS * WAVE) + tid % WAVE;
+    uint32_t key[SEGMENT_KEYS];
+    load_keys(e, j0, key);
+    if (all) {
+        place_kept(e, key, j0, 0, segment * SEGMENT, 0);
+        return;
+    }
+    uint32_t floor_key = 0, equal = e.need;
+    uint32_t before = 0, tied_before = 0;   // of the segments before: keys that stay, keys at floor_key
+    if (PHASE > 0) {
+        if (PHASE > 1) {
+            const uint2 x = b.state[(uint64_t)(PHASE - 2) * (b.all / b.segments) + row];
+            floor_key = x.x;
+            equal = x.y;
+        }
+        const uint32_t *level = b.hist + ((uint64_t)((PHASE - 1) % 2) * b.all + (uint64_t)row * b.segments) * DIGITS;
+        const uint32_t there = (e.cand + SEGMENT - 1) / SEGMENT, digit = DIGITS - 1 - 2 * tid;   // and the one below
+        uint32_t hi = 0, lo = 0, mine_hi = 0, mine_lo = 0;   // mine: this segment's, at last those before it
+#pragma unroll 4
+        for (uint32_t g = 0; g < there; ++g) {
+            const uint2 x = *(const uint2 *)(level + (uint64_t)g * DIGITS + digit - 1);
+            hi += x.y;
+            lo += x.x;
+            const bool count = PHASE < 3 ? g == segment : g < segment;
+            mine_hi += count ? x.y : 0;
+            mine_lo += count ? x.x : 0;
+        }
+        const uint32_t pick = pick_digit(hi, lo, &equal, tmp);
+        floor_key |= pick << digit_shift(PHASE - 1);
+        if (PHASE == 3 && (pick == digit || pick == digit - 1)) tied = pick == digit ? mine_hi : mine_lo;
+        uint32_t above;
+        block_excl_scan((digit > pick ? mine_hi : 0) + (digit - 1 > pick ? mine_lo : 0), tmp, &above);
+        if (PHASE < 3) {
+            if (tid == 0) b.above[(uint64_t)(PHASE - 1) * b.all + blockIdx.x] = above;
+            if (tid == 0 && segment == 0) b.state[(uint64_t)(PHASE - 1) * (b.all / b.segments) + row] = make_uint2(floor_key, equal);
+        } else {
+            before = above;
+            for (uint32_t g = 0; g < segment; ++g)
+                before += b.above[(uint64_t)row * b.segments + g] + b.above[b.all + (uint64_t)row * b.segments + g];
+            tied_before = tied;
+        }
+    }
+    if (PHASE < 3) {
+        count_digits(hist, key, PHASE, floor_key);
+        uint32_t *out = b.hist + ((uint64_t)(PHASE % 2) * b.all + blockIdx.x) * DIGITS;
+        out[tid] = hist[tid];
+        out[tid + SELECT_THREADS] = hist[tid + SELECT_THREADS];
+        return;
+    }
+    place_kept(e, key, j0, floor_key, before + min(tied_before, equal), equal - min(tied_before, equal));
 }
 
 constexpr uint32_t MOVE_SLOTS = 64;   // slots of one (sequence, head) per workgroup
@@ -438,6 +535,20 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t g
         *(uint4 *)(a.kv.k + dst) = x;
         *(uint4 *)(a.kv.v + dst) = y;
     }
+}
+
+static bool evict_split(uint32_t max_kv) { return max_kv > (uint32_t)ROW_KEYS * SELECT_THREADS; }
+static size_t evict_carve(char *ws, uint64_t rows, uint32_t max_kv, int32_t **status, EvictSplit *b) {
+    Carver c{ws, 0};
+    *status = c.take<int32_t>(WS_HEADER / 4);
+    if (evict_split(max_kv)) {
+        b->segments = (max_kv + SEGMENT - 1) / SEGMENT;
+        b->all = rows * b->segments;
+        b->hist = c.take<uint32_t>(2 * b->all * DIGITS);
+        b->above = c.take<uint32_t>(2 * b->all);
+        b->state = c.take<uint2>(2 * rows);
+    }
+    return c.off;
 }
 
 }  // namespace pc
@@ -488,10 +599,9 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
 }
 
 size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv) {
-    (void)n_seqs;
-    (void)n_kv_heads;
-    (void)max_kv;
-    return pc::WS_HEADER;
+    pc::EvictSplit b;
+    int32_t *status;
+    return pc::evict_carve(nullptr, (uint64_t)n_seqs * n_kv_heads, max_kv, &status, &b);
 }
 
 pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
@@ -509,7 +619,8 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     if (n_seqs && (!kv_len || !kept || !new_len || (max_kv && !weight))) return PC_ERR_INVALID;
     if (dst_table && (max_kv > table_stride * a.kv.page || budget > dst_stride * a.kv.page || (max_kv && !page_table)))
         return PC_ERR_INVALID;
-    if (!ws || ws_bytes < pc_kv_evict_ws(n_seqs, a.kv.n_kv, max_kv)) return PC_ERR_WORKSPACE;
+    EvictSplit b;
+    if (!ws || ws_bytes < evict_carve((char *)ws, (uint64_t)n_seqs * a.kv.n_kv, max_kv, &a.status, &b)) return PC_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     a.table = page_table;
@@ -526,13 +637,20 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     a.kept = kept;
     a.new_len = new_len;
     a.weight_out = weight_out;
-    a.status = (int32_t *)ws;
     a.by_piece = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
     const unsigned rows = n_seqs * a.kv.n_kv;
     const uint32_t groups = (budget < max_kv ? budget : max_kv) / MOVE_SLOTS + 1;
     if (dst_table && (uint64_t)rows * groups > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
-    if (max_kv <= 8u * SELECT_THREADS) PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel<8>, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
-    else PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel<0>, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
+    if (evict_split(max_kv)) {
+        if (b.all > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
+        const dim3 grid((unsigned)b.all);
+        PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<0>, grid, dim3(SELECT_THREADS), 0, st, a, b);
+        PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<1>, grid, dim3(SELECT_THREADS), 0, st, a, b);
+        PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<2>, grid, dim3(SELECT_THREADS), 0, st, a, b);
+        PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<3>, grid, dim3(SELECT_THREADS), 0, st, a, b);
+    } else {
+        PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
+    }
     if (dst_table) PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel, dim3(rows * groups), dim3(256), 0, st, a, groups);
     return PC_OK;
 }

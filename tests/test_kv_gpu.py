@@ -321,3 +321,65 @@ def test_append_and_evict_replay_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((k, v, out["kept"], out["weight"]), want))
+
+
+@pytest.mark.parametrize("length", [8192, 8193, 16384, 16385, 32769, 70000])
+@pytest.mark.parametrize("kind", ["zeros", "ties", "odd"])
+def test_evict_ties_over_segments(length, kind):
+    """Long rows are selected in segments; equal weights go to the lowest slots over all of them."""
+    g = torch.Generator().manual_seed(length)
+    kv = np.array([length, length - 5000, 3, 0])
+    w = weights(kind, (4, 2, length), g)
+    cache = pc.PagedCache(*(torch.zeros((1, 2, 64, 16), dtype=BF16, device="cuda") for _ in range(2)))
+    table = torch.zeros((4, (length + 63) // 64), dtype=torch.int32, device="cuda")
+    for budget, recent in ((length // 3, 7), (length - 5000, 100), (length, 0)):
+        got = pc.kv_evict(cache, table, i32(kv), w.cuda(), budget, recent)
+        torch.cuda.synchronize()
+        assert pc.workspace_status(got["ws"]) == 0
+        kept, moved, new_len = kv_plain.evict(w.numpy(), kv, budget, recent)
+        assert np.array_equal(got["new_len"].cpu().numpy(), new_len)
+        assert np.array_equal(got["kept"].cpu().numpy(), kept)
+        nan = np.isnan(moved)
+        assert np.array_equal(np.isnan(got["weight"].cpu().numpy()), nan)
+        assert np.array_equal(got["weight"].cpu().numpy()[~nan], moved[~nan])
+
+
+@pytest.mark.parametrize("n_seqs", [1, 3, 70, 5000])
+@pytest.mark.parametrize("cache,heads,dim", [(BF16, 3, 80), (FP8, 4, 128), (FP8, 1, 16)])
+def test_append_many_rows(n_seqs, cache, heads, dim):
+    """Above 8,192 rows, in sequences of any length, many of them empty; rows without a slot or
+    a page are left out."""
+    r = np.random.default_rng(n_seqs + dim)
+    rows, page = 9001, 24
+    cut = np.sort(r.integers(0, rows + 1, n_seqs - 1))
+    off = np.concatenate([[0], cut, [rows]])
+    new = np.diff(off)
+    kv = new + r.integers(0, 30, n_seqs)
+    g = torch.Generator().manual_seed(n_seqs)
+    table, pages = tables(kv, page, g)
+    lost = 0
+    if n_seqs == 3:
+        kv[1] = max(0, new[1] - 5)                    # its first rows have no slot
+        table[2, 1] = pages + 7                       # no page
+    k, v = (pool(pages, heads, page, dim, cache, g) for _ in range(2))
+    kn, vn = ((torch.randn((rows, heads, dim), generator=g) * 3).to(BF16).cuda() for _ in range(2))
+    scales = [torch.full((heads,), 0.5, device="cuda") if cache == FP8 else None for _ in range(2)]
+    want = []
+    for x, n in ((k, kn), (v, vn)):
+        y = x.detach().cpu().float().numpy().astype(np.float64)
+        z = n.cpu().float().numpy().astype(np.float64)
+        if cache == FP8:
+            z = kv_plain.nearest_e4m3(z / 0.5)
+        for s in range(n_seqs):
+            for i in range(new[s]):
+                j = kv[s] - new[s] + i
+                if j < 0 or table[s, j // page] >= pages:
+                    lost += 1
+                    continue
+                y[table[s, j // page], :, j % page] = z[off[s] + i]
+        want.append(y)
+    ws = pc.kv_append(pc.PagedCache(k, v, *scales), i32(table), i32(kv), i32(off), kn, vn)
+    torch.cuda.synchronize()
+    assert pc.workspace_status(ws) == (2 if lost else 0) and (lost > 0) == (n_seqs == 3)
+    for x, y in zip((k, v), want):
+        assert np.array_equal(x.cpu().float().numpy().astype(np.float64), y)

@@ -2,7 +2,7 @@
  * libpc -- the prefix-cache eviction hot path on one AMD Instinct MI355X
  * (gfx950): chained block hashing, prev/next-use indexing, exact LRU stack
  * distance and the hit-ratio / compute-savings histograms over every cache
- * capacity at once.
+ * capacity at once; and the operators over a paged cache of the blocks.
  *
  * Paper: Y. Liu, M. Yu, J. Yang, "When Fancy Eviction Fails: Rethinking Cache
  * Replacement For LLM Prefix Reuse".  Each entry point cites the passage
@@ -570,7 +570,8 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
  *   dst_table  uint32, [s] rows dst_stride apart of pages with room for `budget` slots, in the
  *              same cache, none of them a page of any of the call's sequences (shared
  *              prefix pages are never written); NULL: nothing is moved
- * With max_kv above 2^31 - 2^16 the call returns PC_ERR_TOO_LARGE. */
+ * With max_kv above 2^31 - 2^16 the call returns PC_ERR_TOO_LARGE.  Above 8192 the
+ * workspace takes 16 KB per (sequence, head) and 16384 slots of max_kv. */
 size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv);
 pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
                       const uint32_t *kv_len, uint32_t n_seqs, uint32_t max_kv, const float *weight,

@@ -625,6 +625,8 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_
     table, stride = _table(page_table, "page_table", n_seqs)
     max_kv = _room(page_table, cache, max_kv)
     dtype, shape = _DTYPES.get(q.dtype), q.shape
+    if window < 0 or max_q < 0:
+        raise PcError("window and max_q: expected at least 0")
     if len(shape) != 3 or dtype is None or shape[2] != cache.head_dim:
         raise PcError("expected q as [rows, heads, %d] of bfloat16 or float16" % cache.head_dim)
     n_rows, n_heads, dim = shape
@@ -668,6 +670,8 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
     {"kept" (int32, -1 behind the last), "weight", "new_len", "ws"}."""
     L = lib()
     n_seqs = kv_len.shape[0]
+    if budget < 1 or not 0 <= recent <= budget:
+        raise PcError("expected a budget of at least 1, and 0 <= recent <= budget")
     table, stride = _table(page_table, "page_table", n_seqs)
     heads = cache.n_kv_heads
     if weight.dtype != torch.float32 or len(weight.shape) != 3 or weight.shape[:2] != (n_seqs, heads):
@@ -684,8 +688,6 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
             raise PcError("dst_table: room for fewer than budget slots")
     shape = (n_seqs, heads, budget)
     if out is None:
-        if budget < 1:
-            raise PcError("budget: expected at least 1")
         out = {"kept": weight.new_empty(shape, dtype=torch.int32), "weight": weight.new_empty(shape),
                "new_len": kv_len.new_empty((n_seqs,))}
     else:

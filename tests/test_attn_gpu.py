@@ -406,3 +406,31 @@ def test_refusals():
         pc.PagedCache(c.kc, c.vc[:, :1])
     with pytest.raises(pc.PcError):
         pc.PagedCache(c.kc.float(), c.vc.float())
+
+
+def test_negative_bounds_are_refused():
+    c = Case([100, 41], [4, 4], heads=8, kvh=2)
+    for kw in (dict(window=-1), dict(max_q=-1), dict(max_kv=-1)):
+        with pytest.raises(pc.PcError):
+            c.run(**kw)
+    cache = pc.PagedCache(c.kc, c.vc)
+    w = torch.zeros(2, 2, 112, device="cuda")
+    for budget, recent in ((-1, 0), (8, -1), (8, 9), (0, 0)):
+        with pytest.raises(pc.PcError):
+            pc.kv_evict(cache, c.d_table, c.d_kv, w, budget, recent)
+
+
+def test_decreasing_lengths_and_many_parts():
+    """Sequences that are cut into ranges among ones that are not, more parts than a join takes at once."""
+    kv = [40, 6000, 10, 3000, 0, 700, 5000]
+    for new in (1, 2, 45):
+        c = Case(kv, [min(new, n) for n in kv], heads=4, kvh=1, dim=128, page=64, weights=True, seed=new)
+        c.check()
+        c.check(window=1000)
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0])
+@pytest.mark.parametrize("cache", ["same", "fp8"])
+def test_weights_of_chunks_with_other_scales(scale, cache):
+    for dim in (80, 128):
+        Case([400, 300], [130, 65], heads=6, kvh=2, dim=dim, cache=FP8 if cache == "fp8" else None, weights=True, seed=dim).check(scale=scale, window=90)

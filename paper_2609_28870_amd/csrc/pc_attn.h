@@ -156,6 +156,7 @@ struct AttnArgs {
     // the work list
     uint32_t target;             // items wanted
     uint32_t least;              // tiles of an item, at least
+    uint32_t cut_first;          // the ranges of sequences that are cut come first: what is left for the end is smaller
     uint32_t row_tile, key_tile; // rows, keys
     uint32_t slots;              // partial results that fit
     uint32_t slot_rows;
@@ -242,8 +243,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
     const uint64_t len = (tiles * a.kv.n_kv + a.target - 1) / a.target;
     it.length = uniform(len > a.least ? (uint32_t)(len < 0x7FFFFFFFu ? len : 0x7FFFFFFFu) : a.least);
     uint64_t base = 0, slot = 0;
-    // the ranges of the sequences that are cut come first: what is left for the end is smaller
-    const int classes = BY == By::SEQ ? 1 : 2;
+    const int classes = BY != By::SEQ && a.cut_first ? 2 : 1;
 #pragma unroll 1
     for (int whole = 0; whole < classes; ++whole) {
         for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
@@ -255,7 +255,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
                 splits = splits ? splits : 1;
                 const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
                 items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
-                if ((splits == 1) == (whole == 1)) count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
+                if (classes == 1 || (splits == 1) == (whole == 1)) count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
             }
             const uint32_t partial = splits > 1 ? items : 0, slot_end = wave_incl_scan(partial);
             const uint32_t end = BY == By::SEQ ? 0 : wave_incl_scan(count);

@@ -1017,6 +1017,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.window = window;
     a.by_16 = a.kv.page % 16 == 0 && a.kv.st < (1u << 24);
     a.target = p.items;
+    a.cut_first = p.items == CHUNK_ITEMS_RAGGED;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);

@@ -317,15 +317,19 @@ __device__ __forceinline__ void place_rest(const EvictArgs &a, const EvictRow &e
         if (e.wout) e.wout[r] = r < e.n ? e.w[j] : 0.f;
     }
 }
-// This thread's keys: slots j0 + 64 i.  Key 0 is no weight's: slots past the candidates.
+// This thread's slots j0 + 64 i: their weights, and the keys that order them.  Key 0 is no
+// weight's: slots past the candidates.
 template <int N>
-__device__ __forceinline__ void load_keys(const EvictRow &e, uint32_t j0, uint32_t (&key)[N]) {
+struct SlotKeys {
     float x[N];
+    uint32_t key[N];
+    __device__ __forceinline__ SlotKeys(const EvictRow &e, uint32_t j0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = e.w[min(j0 + i * WAVE, e.cand - 1)];
+        for (int i = 0; i < N; ++i) x[i] = e.w[min(j0 + i * WAVE, e.cand - 1)];
 #pragma unroll
-    for (int i = 0; i < N; ++i) key[i] = j0 + i * WAVE < e.cand ? order_of(x[i]) : 0;
-}
+        for (int i = 0; i < N; ++i) key[i] = j0 + i * WAVE < e.cand ? order_of(x[i]) : 0;
+    }
+};
 // digit number 0, 1 or 2 of a key, from the top
 __device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
 template <int N>
@@ -356,9 +360,10 @@ __device__ __forceinline__ uint32_t pick_digit(uint32_t hi, uint32_t lo, uint32_
 // The kept ones of a workgroup's keys to their places, from `at` on: those above floor_key, and
 // `quota` at most of those equal to it.  A wave's slots are consecutive, and so are the waves'.
 template <int N>
-__device__ __forceinline__ void place_kept(const EvictRow &e, const uint32_t (&key)[N], uint32_t j0, uint32_t floor_key,
-                                           uint32_t at, uint32_t quota) {
+__device__ __forceinline__ void place_kept(const EvictRow &e, const SlotKeys<N> &slots, uint32_t j0, uint32_t floor_key, uint32_t at,
+                                           uint32_t quota) {
     __shared__ uint32_t above_of[SELECT_WAVES], ties_of[SELECT_WAVES];
+    const uint32_t(&key)[N] = slots.key;
     const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid / WAVE));
     uint32_t above = 0, ties = 0;
 #pragma unroll
@@ -371,16 +376,10 @@ __device__ __forceinline__ void place_kept(const EvictRow &e, const uint32_t (&k
         ties_of[wave] = ties;
     }
     __syncthreads();
-    const uint32_t first = at;
-    uint32_t end = at, left = quota;
-    for (uint32_t i = 0; i < (uint32_t)SELECT_WAVES; ++i) {
-        if (i == wave) {
-            at = end;
-            quota = left;
-        }
-        const uint32_t t = min(ties_of[i], left);
-        end += above_of[i] + t;
-        left -= t;
+    for (uint32_t i = 0; i < wave; ++i) {
+        const uint32_t t = min(ties_of[i], quota);
+        at += above_of[i] + t;
+        quota -= t;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -389,18 +388,12 @@ __device__ __forceinline__ void place_kept(const EvictRow &e, const uint32_t (&k
         const bool keep = (key[i] > floor_key) | (tie & (mbcnt_acc(tied, 0) < quota));
         quota -= min(quota, (uint32_t)__popcll(tied));
         const uint64_t all = ballot(keep);
-        if (keep) e.kept[at + mbcnt_acc(all, 0)] = j0 + i * WAVE;
+        if (keep) {
+            const uint32_t r = at + mbcnt_acc(all, 0);
+            e.kept[r] = j0 + i * WAVE;
+            if (e.wout) e.wout[r] = slots.x[i];
+        }
         at += (uint32_t)__popcll(all);
-    }
-    if (!e.wout) return;
-    __syncthreads();
-    for (uint32_t r0 = first + tid; r0 < end; r0 += 4 * SELECT_THREADS) {
-        float x[4];
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) x[i] = e.w[e.kept[min(r0 + i * SELECT_THREADS, end - 1)]];
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-            if (r0 + i * SELECT_THREADS < end) e.wout[r0 + i * SELECT_THREADS] = x[i];
     }
 }
 
@@ -418,25 +411,24 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
     place_rest(a, e, 0, 1);
     if (!e.need) return;
     const uint32_t tid = threadIdx.x, j0 = tid / WAVE * (ROW_KEYS * WAVE) + tid % WAVE;
-    uint32_t key[ROW_KEYS];
-    load_keys(e, j0, key);
+    const SlotKeys<ROW_KEYS> slots(e, j0);
     uint32_t floor_key = 0, equal = 0;   // keys above floor_key stay, and `equal` of those at it
     if (e.need < e.cand) {
         equal = e.need;
 #pragma unroll 1   // small code: of a few-microsecond call much is the first fetch of its instructions
         for (int digit = 0; digit < 3; ++digit) {
-            count_digits(hist, key, digit, floor_key);
+            count_digits(hist, slots.key, digit, floor_key);
             floor_key |= pick_digit(hist[DIGITS - 1 - 2 * tid], hist[DIGITS - 2 - 2 * tid], &equal, tmp) << digit_shift(digit);
         }
     }
-    place_kept(e, key, j0, floor_key, 0, equal);
+    place_kept(e, slots, j0, floor_key, 0, equal);
 }
 
 // Longer rows: a workgroup per segment of 16384 slots, and a launch per digit, since
 // the segments have to meet: each phase adds up its row's histograms of the digit before
 // and counts the next; the last one places.  What a segment needs to know of those
 // before it (the keys above the digit) follows from their histograms.
-// 16 sequences of 4 heads, 303k slots, the longest 65,536: 32 us in four launches (one workgroup a row: 60, keys
+// 16 sequences of 4 heads, 303k slots, the longest 65,536: 33 us in four launches (one workgroup a row: 60, keys
 // in registers, or 71).
 constexpr int SEGMENT_KEYS = 16;
 constexpr uint32_t SEGMENT = SEGMENT_KEYS * SELECT_THREADS;
@@ -459,10 +451,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_split_kernel(EvictArgs a
     const bool all = e.need == e.cand;
     if (PHASE < 3 && all) return;
     const uint32_t j0 = segment * SEGMENT + tid / WAVE * (SEGMENT_KEYS * WAVE) + tid % WAVE;
-    uint32_t key[SEGMENT_KEYS];
-    load_keys(e, j0, key);
+    const SlotKeys<SEGMENT_KEYS> slots(e, j0);
     if (all) {
-        place_kept(e, key, j0, 0, segment * SEGMENT, 0);
+        place_kept(e, slots, j0, 0, segment * SEGMENT, 0);
         return;
     }
     uint32_t floor_key = 0, equal = e.need;
@@ -501,13 +492,13 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_split_kernel(EvictArgs a
         }
     }
     if (PHASE < 3) {
-        count_digits(hist, key, PHASE, floor_key);
+        count_digits(hist, slots.key, PHASE, floor_key);
         uint32_t *out = b.hist + ((uint64_t)(PHASE % 2) * b.all + blockIdx.x) * DIGITS;
         out[tid] = hist[tid];
         out[tid + SELECT_THREADS] = hist[tid + SELECT_THREADS];
         return;
     }
-    place_kept(e, key, j0, floor_key, before + min(tied_before, equal), equal - min(tied_before, equal));
+    place_kept(e, slots, j0, floor_key, before + min(tied_before, equal), equal - min(tied_before, equal));
 }
 
 constexpr uint32_t MOVE_SLOTS = 64;   // slots of one (sequence, head) per workgroup

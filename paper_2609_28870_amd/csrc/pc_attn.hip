@@ -303,22 +303,25 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
 
 // ------------------------------------------------------------------ chunks
 
-constexpr int CHUNK_ROWS = 128;
+constexpr int CHUNK_WAVES = 4, CHUNK_WAVES_WIDE = 8;
 // keys of a tile: with 256 dimensions half as many, so that the registers hold out
 constexpr __host__ __device__ int chunk_keys(int d) { return d <= 128 ? 64 : 32; }
 
-// 128 rows against a range of keys, 32 rows a wave, in tiles of 64 keys that the
-// workgroup shares through LDS (two buffers: the next tile is loaded to
-// registers while this one is worked on, and written to the other buffer).
+// 32 rows a wave against a range of keys, in tiles of 64 keys that the workgroup
+// shares through LDS (two buffers: the next tile is loaded to registers while this one is
+// worked on, and written to the other buffer).  W waves: four and two workgroups to a
+// compute unit, or eight, which load and write half as much a wave for rows that last.
 // Bound by the matrix products and the exponentials between them: 2,048 tokens over
-// 32,768 (bf16, 32 over 4 heads of 128) 1,160 to 1,230 us, 870 to 920 TFLOP/s, the matrix
-// cores busy 41% of the cycles and vector instructions issued in 42%.
-template <class T, bool F8, int D, bool FULL>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
+// 32,768 (bf16, 32 over 4 heads of 128) 1,050 us, 1,014 TFLOP/s (four waves: 1,141); the
+// matrix cores are busy in 43% of the cycles, vector instructions issued in 42%.
+template <class T, bool F8, int D, bool FULL, int W>
+__global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
+    constexpr int THREADS = W * WAVE, ROWS = 32 * W;
     constexpr int CHUNK_KEYS = chunk_keys(D), BLOCKS = CHUNK_KEYS / 32;
     constexpr int PER_ROW = F8 ? D / 16 : D / 8;            // 16-byte pieces of a cache entry
-    constexpr int PIECES = CHUNK_KEYS * PER_ROW / 256;      // of one thread
+    constexpr int PIECES = CHUNK_KEYS * PER_ROW / THREADS;      // of one thread
     constexpr int TILE = CHUNK_KEYS * D * 2;
+    static_assert(PIECES * THREADS == CHUNK_KEYS * PER_ROW, "whole pieces");
     __shared__ __attribute__((aligned(16))) char lds[2][2][TILE];
     __shared__ uint32_t odd;   // a value that is not finite was left out of a tile
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     if (!it.there) return;
     const uint32_t tid = threadIdx.x, lane = tid & (WAVE - 1), half = lane / 32, wave = uniform(tid / WAVE), col = lane % 32;
     const Seq &sq = it.shape.q;
-    const uint32_t rows = sq.rows * a.group, r0 = it.row_tile * CHUNK_ROWS, row = r0 + wave * 32 + col;
+    const uint32_t rows = sq.rows * a.group, r0 = it.row_tile * ROWS, row = r0 + wave * 32 + col;
     uint32_t flip;
     bool zero;
     const float c = score_factor(a, it.head, &flip, &zero);
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
     all_first = (int32_t)uniform((uint32_t)all_first);
     all_last = (int32_t)uniform((uint32_t)all_last);
     // the tile's own keys, and those that all its rows see, inside the item's range
-    const uint32_t i0 = a.by_group.div(r0), i1 = a.by_group.div(min(r0 + CHUNK_ROWS, rows) - 1);
+    const uint32_t i0 = a.by_group.div(r0), i1 = a.by_group.div(min(r0 + ROWS, rows) - 1);
     const Range own = seen(a, sq, i0, i1);
     int32_t wg_first, wg_last, unused;
     seen_by_row(a, sq, i1, &wg_first, &unused);
@@ -370,7 +373,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
         if (a.by_16) return;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t j = min(k0 + (tid + 256 * i) / PER_ROW, k_hi - 1), p = a.kv.by_page.div(j);
+            const uint32_t j = min(k0 + (tid + THREADS * i) / PER_ROW, k_hi - 1), p = a.kv.by_page.div(j);
             off[i] = j - p * a.kv.page;
             entry[i] = table[p];
         }
@@ -384,7 +387,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
             }
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const uint32_t r = (wave * WAVE + 256 * i) / PER_ROW, g = min(k0 / 16 + r / 16, g_last), slot = g * 16;
+                const uint32_t r = (wave * WAVE + THREADS * i) / PER_ROW, g = min(k0 / 16 + r / 16, g_last), slot = g * 16;
                 const uint32_t p = a.kv.by_page.div(slot);
                 const uint32_t page = page_of(a.kv, from_lane(groups, (int)(g - g0)));
                 const uint64_t at = entry_at(a.kv, page, slot - p * a.kv.page + r % 16, it.head);
@@ -414,11 +417,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             // rows a multiple of 16 on have the same spread, those 8 on another by 2
-            const uint32_t at = 256 / PER_ROW * i * D * 2, turn = 256 / PER_ROW == 8 && i % 2 ? 32 : 0;
+            const uint32_t at = THREADS / PER_ROW * i * D * 2, turn = THREADS / PER_ROW == 8 && i % 2 ? 32 : 0;
             auto put = [&](uint4 x, uint4 y, int e) {
                 if (past_dim) x = make_uint4(0, 0, 0, 0);
                 if (edge) {   // slots past the end may hold anything
-                    if (k0 + (tid + 256 * i) / PER_ROW >= k_hi) y = make_uint4(0, 0, 0, 0);
+                    if (k0 + (tid + THREADS * i) / PER_ROW >= k_hi) y = make_uint4(0, 0, 0, 0);
                     y = drop_not_finite<T>(y, &mine);
                 }
                 const uint32_t o = (to[e] ^ turn) + at;
@@ -860,17 +863,20 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(AttnArgs a, uint32_t ke
 
 constexpr uint32_t ROWS_MOST = 32;           // rows of the path for few rows
 constexpr uint32_t ROWS_ITEMS = 1024;
-// Two workgroups of chunk_kernel fit a compute unit: 512 items are one round of them.  Of
-// a few sequences they come out alike; of several, uneven lengths leave gaps that
-// smaller items fill (12 ragged chunks: 227 to 197 us), which costs a join where there
-// was none (one chunk of 2,048 over 32,768: 18 us of 1,160).
-constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
+// Chunks: one round of the chip, 512 workgroups of four waves, or 256 of eight.  The wide
+// ones take few sequences of many rows over long caches in heads of 65 to 128 dimensions
+// (2,048 tokens over 32,768: 1,050 us, 1,141 narrow; 128 over 32,768: 96, 99; but 2,048 over
+// 4,096: 148, 140, and 12 ragged chunks: 230, 195).  Of several sequences, uneven
+// lengths leave gaps that smaller items fill (12 ragged chunks: 227 to 197 us), which
+// costs a join where there was none (one chunk of 2,048 over 32,768: 18 us).
+constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_WIDE = 256, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
+constexpr uint32_t WIDE_ROWS = 1024, WIDE_KEYS = 8192;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
 constexpr uint32_t WEIGHT_ITEMS = 4096;   // with 1024, two rounds of the chip, uneven ends took a quarter of the time
 
 struct AttnPlan {
-    bool few;
-    uint32_t dim, items, slots, slot_rows, weight_parts, key_blocks;
+    bool few, wide;
+    uint32_t row_tile, dim, items, slots, slot_rows, weight_parts, key_blocks;
     uint64_t score_stride;
 };
 static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim) {
@@ -879,9 +885,11 @@ static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint
     p.few = (uint64_t)max_q * group <= ROWS_MOST;
     p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
     // an item that is a part has more than half an item's tiles: at most two per item wanted
-    p.items = p.few ? ROWS_ITEMS : n_seqs < RAGGED_SEQS ? CHUNK_ITEMS : CHUNK_ITEMS_RAGGED;
+    p.wide = !p.few && p.dim == 128 && n_seqs < RAGGED_SEQS && (uint64_t)max_q * group >= WIDE_ROWS && max_kv >= WIDE_KEYS;
+    p.row_tile = p.few ? ROWS_MOST : 32 * (p.wide ? CHUNK_WAVES_WIDE : CHUNK_WAVES);
+    p.items = p.few ? ROWS_ITEMS : p.wide ? CHUNK_ITEMS_WIDE : n_seqs < RAGGED_SEQS ? CHUNK_ITEMS : CHUNK_ITEMS_RAGGED;
     p.slots = 2 * p.items;
-    p.slot_rows = p.few ? (max_q ? max_q : 1) * group : CHUNK_ROWS;
+    p.slot_rows = p.few ? (max_q ? max_q : 1) * group : p.row_tile;
     p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
     p.key_blocks = (uint32_t)(((uint64_t)max_kv + WEIGHT_KEYS - 1) / WEIGHT_KEYS);
     const uint64_t blocks = (uint64_t)n_seqs * n_kv * (p.key_blocks ? p.key_blocks : 1);
@@ -918,8 +926,11 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, 
     if (p.few) {
         if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
         else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, false>), items, dim3(256), 0, st, a);
+    } else if (p.wide) {
+        constexpr int W = D == 128 ? CHUNK_WAVES_WIDE : CHUNK_WAVES;
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL, W>), items, dim3(W * WAVE), 0, st, a);
     } else {
-        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL>), items, dim3(256), 0, st, a);
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
     }
     // few joins take several teams to a row (a decode batch: 8.7 us in 1,008 workgroups, 13 in
     // 2,016); many are walked by at most 2048 workgroups, or one
@@ -1019,11 +1030,11 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.target = p.items;
     a.cut_first = p.items == CHUNK_ITEMS_RAGGED;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
-    a.row_tile = p.few ? ROWS_MOST : CHUNK_ROWS;
+    a.row_tile = p.row_tile;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     // tiles of rows of every head, at most
-    const uint64_t tiles = (p.few ? n_seqs : (uint64_t)n_rows * a.group / CHUNK_ROWS + n_seqs) * (uint64_t)a.kv.n_kv;
+    const uint64_t tiles = (p.few ? n_seqs : (uint64_t)n_rows * a.group / p.row_tile + n_seqs) * (uint64_t)a.kv.n_kv;
     if (tiles * p.slot_rows + a.target > 0x7FFFFFFFu || (uint64_t)n_seqs * a.kv.n_kv * ((uint64_t)p.key_blocks + 1) * 16 > 0x7FFFFFFFu)
         return PC_ERR_TOO_LARGE;
     const bool f8 = cache->dtype == PC_FP8_E4M3;

@@ -434,3 +434,25 @@ def test_decreasing_lengths_and_many_parts():
 def test_weights_of_chunks_with_other_scales(scale, cache):
     for dim in (80, 128):
         Case([400, 300], [130, 65], heads=6, kvh=2, dim=dim, cache=FP8 if cache == "fp8" else None, weights=True, seed=dim).check(scale=scale, window=90)
+
+
+@pytest.mark.parametrize("dim,page", [(80, 24), (96, 16), (128, 16), (128, 10)])
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, FP8)], ids=["bf16", "f16", "fp8"])
+def test_few_sequences_of_many_rows(dim, page, dtype, cache):
+    """From 1,024 rows (tokens times heads of a group) on, with room for 8,192 slots, tiles of rows
+    are twice as tall."""
+    for kv, new, window in (([1300, 9], [150, 9], 0), ([150], [150], 0), ([2100, 140, 700], [129, 140, 1], 300)):
+        c = Case(kv, new, heads=16, kvh=2, dim=dim, page=page, dtype=dtype, cache=cache, weights=True, seed=dim + page,
+                 cols=8192 // page + 1)
+        c.check(window=window)
+    c.check(causal=False)
+
+
+def test_many_rows_do_not_see_what_is_masked():
+    c = Case([400], [160], heads=8, kvh=1, dim=128, page=16, seed=5, cols=512)
+    for j in (399, 250, 300):
+        page, off = int(c.table[0, j // 16]), j % 16
+        c.vc[page, 0, off, 3 + j % 7] = float("nan") if j % 2 else float("inf")
+    page, off = int(c.table[0, 390 // 16]), 390 % 16
+    c.kc[page, 0, off, 7] = float("nan")
+    c.check()

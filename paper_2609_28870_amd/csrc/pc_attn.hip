@@ -676,7 +676,7 @@ constexpr int WEIGHT_KEYS = 256, WEIGHT_ROWS = 64;
 // passing through LDS.  With the statistics known there is no running maximum: a
 // register holds one row, so a key's sum is a sum over registers.  Bound by the
 // matrix products and exponentials: 2 x 1,024 tokens over 16,384 (bf16, 32 over 4 heads of
-// 128) 390 us, 680 TFLOP/s; the attention before it, of twice the products, 600 to 680.
+// 128) 390 us, 680 TFLOP/s; the attention before it, of twice the products, takes 520.
 template <class T, bool F8, int D, bool FULL>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs a, uint32_t key_blocks) {
     constexpr int PIECES = D / 8 * WEIGHT_ROWS / 256;

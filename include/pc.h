@@ -529,8 +529,10 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  *     weight_out[s][h][j] = weight[s][h][j] + sum over the chunk's rows and the
  *                           heads that share h of exp(s_j - lse)
  * Query head e reads key/value head e / (n_heads / n_kv_heads).  A row that sees
- * nothing has out = 0 and lse = -infinity and adds no weight.  What a row does not
- * see never reaches its outputs, whatever its values.
+ * nothing, or whose every score is -infinity, has out = 0 and lse = -infinity and
+ * adds no weight.  A score that is NaN makes the row's out and lse NaN, and the weights
+ * of the slots that the row sees.  What a row does not see never reaches its outputs,
+ * whatever its values.
  *
  *   q, out     `dtype` PC_BF16 or PC_F16 (the cache the same or PC_FP8_E4M3), head e of
  *              row t at element t * stride_row + e * stride_head; pointers and

@@ -66,6 +66,14 @@ __device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs
         }
 }
 
+// log2 of a row's sum of exponentials, from its maximum and its sum relative to that.  A sum of
+// zero is a row that sees nothing (or scores of -inf alone); the maximum does not say so:
+// it passes over NaN, which is in the sum.
+template <class T>
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l == 0.f ? MINUS_INF : m + __log2f(l) - T::TOP;
+}
+
 // A row's result: whole (its sequence is one item long), or a part for the join.
 template <class T, int D>
 __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, const f32x16 (&o)[D / 32], float m, float l,
@@ -82,8 +90,8 @@ __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, co
                     make_float4(o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]);
         return;
     }
-    const float base2 = m == MINUS_INF ? MINUS_INF : m + __log2f(l) - T::TOP;
-    const float f = m == MINUS_INF ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / l;
+    const float base2 = log_sum<T>(m, l);
+    const float f = l == 0.f ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / l;
     if (half == 0) {
         if (a.lse) a.lse[(uint64_t)t * a.n_heads + head] = base2 * LN2;
         if (a.lse2) a.lse2[(uint64_t)t * a.n_heads + head] = base2;
@@ -537,7 +545,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
                                                    uint32_t key_blocks) {
     constexpr uint32_t LANES = D / 4, ALL = 256 / LANES;
     __shared__ float4 sums[256];
-    __shared__ float2 stats[32];
+    __shared__ float stats[32];
+    __shared__ int2 sees[32];   // first and last slot
     const uint32_t tid = threadIdx.x;
     if (blockIdx.x < joins) {
         // status
@@ -567,8 +576,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
             const bool there = from + at / teams < rows;
             const uint32_t row = there ? from + at / teams : from;
             const uint32_t part0 = slot_of(a, it, it.head, it.row_tile, 0), apart = it.shape.row_tiles * a.kv.n_kv;
-            // four parts from p on, every teams-th: a part that is not there or saw nothing has the
-            // maximum -inf, and one that saw nothing holds zeros
+            // four parts from p on, every teams-th: one that saw nothing has the maximum -inf and holds
+            // zeros, and so does one that is not there
             auto parts = [&](uint32_t p, float2 (&y)[4], float4 (&x)[4]) {
 #pragma unroll
                 for (uint32_t u = 0; u < 4; ++u) {
@@ -576,16 +585,18 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
                     const uint64_t i = (uint64_t)min(slot, a.slots - 1) * a.slot_rows + row;
                     y[u] = a.part_ml[i];
                     x[u] = *(const float4 *)(a.part + i * D + lane * 4);
-                    if (p + u * teams >= it.splits || slot >= a.slots) y[u].x = MINUS_INF;
+                    if (p + u * teams >= it.splits || slot >= a.slots) {
+                        y[u] = make_float2(MINUS_INF, 0.f);
+                        x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
                 }
             };
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             auto add = [&](const float2 (&y)[4], const float4 (&x)[4], float ref) {
 #pragma unroll
                 for (uint32_t u = 0; u < 4; ++u) {
-                    const float f = exp2_fast(y[u].x - ref);
-                    if (y[u].x != MINUS_INF)
-                        sum = make_float4(sum.x + x[u].x * f, sum.y + x[u].y * f, sum.z + x[u].z * f, sum.w + x[u].w * f);
+                    const float f = exp2_fast(y[u].x - ref);   // 0 for a part whose scores are all NaN: 0 * NaN stays NaN
+                    sum = make_float4(sum.x + x[u].x * f, sum.y + x[u].y * f, sum.z + x[u].z * f, sum.w + x[u].w * f);
                 }
             };
             float2 ml, y[4];
@@ -595,8 +606,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
                 ml = make_float2(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), 0.f);
                 const float ref = ml.x == MINUS_INF ? 0.f : ml.x;
 #pragma unroll
-                for (uint32_t u = 0; u < 4; ++u)
-                    if (y[u].x != MINUS_INF) ml.y += y[u].y * exp2_fast(y[u].x - ref);
+                for (uint32_t u = 0; u < 4; ++u) ml.y += y[u].y * exp2_fast(y[u].x - ref);
                 add(y, x, ref);
             } else {
                 ml = join_stats(a, it, it.head, it.row_tile, row, lane, LANES);
@@ -616,9 +626,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
                 const float4 x = sums[tid + i * LANES];
                 sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
             }
-            const bool none = ml.x == MINUS_INF;
-            const float f = none ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / ml.y;
-            const float base2 = none ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+            const float f = ml.y == 0.f ? 0.f : (a.kv.v_scale ? a.kv.v_scale[it.head] : 1.f) / ml.y;
+            const float base2 = log_sum<T>(ml.x, ml.y);
             const uint32_t i = a.by_group.div(r0 + row), t = it.shape.q.first + i, e = it.head * a.group + (r0 + row - i * a.group);
             if (lane == 0) {
                 if (a.lse) a.lse[(uint64_t)t * a.n_heads + e] = base2 * LN2;
@@ -638,16 +647,18 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
     const uint32_t rows = q.rows * a.group;
     const uint32_t r = tid / 8;   // 32 teams of 8
     if (r < rows) {
+        const uint32_t i = a.by_group.div(r);
         float base2;
         if (it.splits > 1) {
             const float2 ml = join_stats(a, it, h, 0, r, tid % 8, 8);
-            base2 = ml.x == MINUS_INF ? MINUS_INF : ml.x + __log2f(ml.y) - T::TOP;
+            base2 = log_sum<T>(ml.x, ml.y);
         } else {
-            const uint32_t i = a.by_group.div(r);
             base2 = a.lse2[(uint64_t)(q.first + i) * a.n_heads + h * a.group + (r - i * a.group)];
         }
-        // a row that sees nothing adds exp2(-inf - inf) = 0
-        if (tid % 8 == 0) stats[r].x = base2 == MINUS_INF ? __builtin_inff() : base2;
+        if (tid % 8 == 0) {
+            stats[r] = base2 == MINUS_INF ? __builtin_inff() : base2;   // a row without a weight: exp2(-inf)
+            seen_by_row(a, q, i, &sees[r].x, &sees[r].y);
+        }
     }
     __syncthreads();
     const uint64_t row = (uint64_t)s * a.kv.n_kv + h;
@@ -659,7 +670,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
                 const float *x = a.scores + row * a.slot_rows * a.score_stride + j;
                 float sum = 0.f;
 #pragma unroll 8
-                for (uint32_t i = 0; i < rows; ++i) sum += exp2_fast(x[i * a.score_stride] - stats[i].x);
+                for (uint32_t i = 0; i < rows; ++i) {
+                    const float e = exp2_fast(x[i * a.score_stride] - stats[i]);   // NaN of a broken row: for what it sees
+                    sum += ((int32_t)j >= sees[i].x) & ((int32_t)j <= sees[i].y) ? e : 0.f;
+                }
                 w += sum;
             }
         }

@@ -323,9 +323,14 @@ __device__ __forceinline__ void load_query(const AttnArgs &a, const char *row, b
     }
 }
 
+// SLACK in units of scores that are taken times c > 0; finite, so that a first score always
+// passes a maximum of -inf by it
+template <class T>
+__device__ __forceinline__ float slack_of(float c) { return fminf(T::SLACK / c, 3e38f); }
+
 // softmax state of the rows of a wave: lane % 32 is the row; the maximum is
 // common to both halves, the sum is each half's own until the end.  Scores are taken
-// times c, and `slack` is SLACK / c.
+// times c, and `slack` is slack_of(c).
 template <class T, int D>
 struct Rows {
     f32x16 o[D / 32];

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
     bool odd = false;   // a value that is not finite was left out of a tile
     const RowAt<D> q_at;
     const ValueAt<D> v_at;
-    const float slack = T::SLACK / c;
+    const float slack = slack_of<T>(c);
     auto query = [&](int i) { return q_at.read(queries, i); };
     for (; t < t_end; t += 4) {
         const bool more = t + 4 < t_end;
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
     };
     const RowAt<D> k_at;
     const ValueAt<D> v_at;
-    const float slack = T::SLACK / c;
+    const float slack = slack_of<T>(c);
     Rows<T, D> state;
     state.clear();
     if (k_lo < k_hi) {

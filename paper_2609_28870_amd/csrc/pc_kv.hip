@@ -65,15 +65,19 @@ __device__ void append_status(const AppendArgs &a) {
     for (uint32_t s0 = wave * WAVE; s0 < a.n_seqs; s0 += waves * WAVE) {
         const uint32_t s = s0 + lane;
         uint32_t from = 0, pages = 0;
+        bool bad = false;
         if (s < a.n_seqs) {
-            bool bad;
             const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
-            any |= bad || q.rows > q.len;
+            bad |= q.rows > q.len;
             if (q.rows && q.len) {
                 from = a.kv.by_page.div(q.rows < q.len ? q.len - q.rows : 0);
                 pages = a.kv.by_page.div(q.len - 1) + 1 - from;
             }
         }
+        any |= bad;
+        // Pages are counted in 32 bits, which rows that overlap (offsets that decrease) could pass, and
+        // the loop below would not end; but then the status is known.
+        if (ballot(bad)) continue;
         const uint32_t end = wave_incl_scan(pages), all = (uint32_t)__shfl((int)end, WAVE - 1, WAVE);
         for (uint32_t p0 = 0; p0 < all; p0 += WAVE) {
             const uint32_t p = p0 + lane;

@@ -1,8 +1,10 @@
 """The operators over a paged cache at the ends of their arguments' ranges."""
+import numpy as np
 import pytest
 import torch
 
 from test_attn_gpu import BF16, F16, FP8, Case
+from paper_2609_28870_amd import pc
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +30,33 @@ def test_scales_next_to_zero(new):
     c = Case([100, 41, 3000], [new] * 3, cache=FP8, weights=True, seed=4)
     c.ks[0], c.ks[1] = 1.2e-38, -1e-41
     c.check()
+
+
+@pytest.mark.parametrize("new", [1, 200])
+def test_append_beside_offsets_that_decrease(new):
+    """Offsets that decrease in one batch of 64 sequences are reported; the rows of the others, whose
+    pages a batch checks together, go where they belong, and a page too many there is reported too."""
+    n, page, dim = 150, 16, 16
+    off = np.arange(n + 1) * new
+    each = (new + page - 1) // page
+    table = np.arange(n * each).reshape(n, each)
+    rows = torch.randn((n * new, 1, dim), device="cuda").to(BF16)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")   # noqa: E731
+
+    def run(off, table):
+        k = torch.zeros((n * each, 1, page, dim), dtype=BF16, device="cuda")
+        v = torch.zeros_like(k)
+        ws = pc.kv_append(pc.PagedCache(k, v), i32(table), i32([new] * n), i32(off), rows, rows)
+        torch.cuda.synchronize()
+        assert torch.equal(k, v)
+        return pc.workspace_status(ws), k.transpose(1, 2).reshape(n, each * page, 1, dim)
+    code, right = run(off, table)
+    assert code == 0 and torch.equal(right[:, :new], rows.view(n, new, 1, dim)) and not bool(right[:, new:].any())
+    wrong = off.copy()
+    wrong[70], wrong[71] = wrong[71], wrong[70]
+    code, got = run(wrong, table)
+    assert code == 2 and torch.equal(got[:69], right[:69]) and torch.equal(got[72:], right[72:])
+    for s in (0, 63, 64, 127, 128, n - 1):
+        past = table.copy()
+        past[s, -1] = n * each
+        assert run(off, past)[0] == 2

@@ -96,6 +96,13 @@ __device__ void append_status(const AppendArgs &a) {
     if (threadIdx.x == 0) *a.status = wrong;
 }
 
+// slot of row t of sequence s, negative if it has none: by the length as it is, so that one above
+// max_kv moves no row to another's slot
+__device__ __forceinline__ int64_t slot_of_row(const AppendArgs &a, uint32_t s, const Seq &q, uint32_t t) {
+    const int64_t slot = (int64_t)a.kv_len[s] - q.rows + (t - q.first);
+    return slot < (int64_t)a.max_kv ? slot : -1;
+}
+
 __device__ __forceinline__ float to_float(uint32_t bits, bool bf16) {
     if (bf16) return __uint_as_float(bits << 16);
     return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
@@ -131,7 +138,7 @@ __global__ __launch_bounds__(256) void append_few_kernel(AppendArgs a) {
     bool bad;
     const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
     if (t < q.first || t - q.first >= q.rows) return;
-    const int64_t slot = (int64_t)q.len - q.rows + (t - q.first);
+    const int64_t slot = slot_of_row(a, s, q, t);
     if (slot < 0) return;
     const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;
     const uint32_t page = a.table[(uint64_t)s * a.table_stride + at];
@@ -203,7 +210,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             while (s + 1 < a.n_seqs && a.q_off[s + 1] <= t) ++s;
             bool bad;
             const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
-            const int64_t slot = (int64_t)q.len - q.rows + (t - q.first);
+            const int64_t slot = slot_of_row(a, s, q, t);
             there[u] = p < rows * a.pieces && t >= q.first && t - q.first < q.rows && slot >= 0;
             if (!there[u]) continue;
             const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;

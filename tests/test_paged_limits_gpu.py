@@ -60,3 +60,26 @@ def test_append_beside_offsets_that_decrease(new):
         past = table.copy()
         past[s, -1] = n * each
         assert run(off, past)[0] == 2
+
+
+@pytest.mark.parametrize("most,long", [(32, 40), (300, 9000)])
+def test_append_past_the_bound_writes_no_other_slot(most, long):
+    """A length above max_kv is reported: of its new rows those below max_kv go where they
+    belong, the others nowhere."""
+    page, dim, kv, new = 16, 32, [long, 20], [long - most + 4, 2]
+    pages = (long + page - 1) // page + 2
+    table = np.zeros((2, pages - 2), np.int64)
+    table[0], table[1, :2] = np.arange(pages - 2), [pages - 2, pages - 1]
+    g = torch.Generator().manual_seed(long)
+    rows = [torch.randn((sum(new), 2, dim), generator=g).to(BF16).cuda() for _ in range(2)]
+    k, v = (torch.zeros((pages, 2, page, dim), dtype=BF16, device="cuda") for _ in range(2))
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")   # noqa: E731
+    ws = pc.kv_append(pc.PagedCache(k, v), i32(table), i32(kv), i32([0, new[0], sum(new)]), *rows, max_kv=most)
+    torch.cuda.synchronize()
+    assert pc.workspace_status(ws) == 2
+    for x, r in zip((k, v), rows):
+        slots = x.transpose(1, 2).reshape(-1, 2, dim)
+        want = torch.zeros_like(slots)
+        want[most - 4:most] = r[:4]
+        want[(pages - 2) * page + 18:(pages - 2) * page + 20] = r[new[0]:]
+        assert torch.equal(slots, want)

@@ -176,7 +176,7 @@ struct Range {
     uint32_t lo, hi;
 };
 __device__ __forceinline__ Range seen(const AttnArgs &a, const Seq &q, uint32_t i0, uint32_t i1) {
-    const int64_t j0 = (int64_t)q.len - q.rows;
+    const int64_t j0 = q.slot;
     int64_t hi = a.causal ? j0 + i1 + 1 : (int64_t)q.len, lo = a.window ? j0 + i0 - (int64_t)a.window + 1 : 0;
     if (hi > (int64_t)q.len) hi = q.len;
     if (lo < 0) lo = 0;
@@ -185,7 +185,7 @@ __device__ __forceinline__ Range seen(const AttnArgs &a, const Seq &q, uint32_t 
 }
 // slots that row i sees: first .. last (none if last < first)
 __device__ __forceinline__ void seen_by_row(const AttnArgs &a, const Seq &q, uint32_t i, int32_t *first, int32_t *last) {
-    const int64_t x = (int64_t)q.len - q.rows + i;
+    const int64_t x = (int64_t)q.slot + i;
     const int64_t lo = a.window ? x - (int64_t)a.window + 1 : 0;
     *first = lo > 0 ? (lo < 0x7FFFFFFF ? (int32_t)lo : 0x7FFFFFFF) : 0;
     *last = a.causal && x < (int64_t)q.len ? (x < 0 ? -1 : (int32_t)x) : (int32_t)q.len - 1;
@@ -206,7 +206,7 @@ __device__ __forceinline__ Shape shape_of(const AttnArgs &a, uint32_t s) {
     Shape h;
     bool bad;
     h.q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
-    if (h.q.rows > a.max_q) h.q.rows = a.max_q;
+    if (h.q.rows > a.max_q) h.q.rows = a.max_q;   // the first ones, at the slots that they have
     h.keys = h.q.rows ? seen(a, h.q, 0, h.q.rows - 1) : Range{0, 0};
     h.keys.lo &= ~(a.key_tile - 1);   // a power of two
     h.row_tiles = (uint32_t)(((uint64_t)h.q.rows * a.group + a.row_tile - 1) / a.row_tile);
@@ -270,6 +270,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
                 it.shape.q.first = from_lane(h.q.first, at);
                 it.shape.q.rows = from_lane(h.q.rows, at);
                 it.shape.q.len = from_lane(h.q.len, at);
+                it.shape.q.slot = (int32_t)from_lane((uint32_t)h.q.slot, at);
                 it.shape.keys.lo = from_lane(h.keys.lo, at);
                 it.shape.keys.hi = from_lane(h.keys.hi, at);
                 it.shape.row_tiles = from_lane(h.row_tiles, at);

@@ -715,7 +715,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
     const uint32_t k_lo = max(k0, shape.keys.lo), k_hi = min(min(k0 + WEIGHT_KEYS, shape.keys.hi), q.len);
     if (k_lo < k_hi) {
         // rows (token, head of the group) that see any of the keys, and this part of them
-        const int64_t j0 = (int64_t)q.len - q.rows;
+        const int64_t j0 = q.slot;
         int64_t i_lo = a.causal ? (int64_t)k_lo - j0 : 0, i_hi = a.window ? (int64_t)k_hi - 1 + a.window - j0 : q.rows;
         i_lo = i_lo < 0 ? 0 : i_lo > (int64_t)q.rows ? (int64_t)q.rows : i_lo;
         i_hi = i_hi < i_lo ? i_lo : i_hi > (int64_t)q.rows ? (int64_t)q.rows : i_hi;

@@ -30,17 +30,20 @@ struct KvView {
 pc_status kv_view(const pc_kv_cache *c, KvView *v);   // checks the descriptor
 size_t type_size(uint32_t dtype);                     // 0: no such type
 
-// Rows of sequence s inside the chunk arrays, and its length; a table entry
-// that does not fit (decreasing, past n_q) counts as no rows.
+// Rows of sequence s inside the chunk arrays, its length, and the slot of its first row
+// (negative: rows before slot 0); a table entry that does not fit (decreasing, past n_q)
+// counts as no rows.
 struct Seq {
     uint32_t first, rows, len;
+    int32_t slot;
 };
 __device__ __forceinline__ Seq load_seq(const uint32_t *__restrict__ q_off, const uint32_t *__restrict__ kv_len, uint32_t s,
                                         uint32_t n_q, uint32_t max_kv, bool *bad) {
     const uint32_t a = q_off[s], b = q_off[s + 1], l = kv_len[s];
     const bool ok = a <= b && b <= n_q;
     *bad = !ok || l > max_kv;
-    return Seq{a, ok ? b - a : 0u, l < max_kv ? l : max_kv};
+    const uint32_t rows = ok ? b - a : 0u, len = l < max_kv ? l : max_kv;
+    return Seq{a, rows, len, (int32_t)(len - rows)};
 }
 
 // sequence of chunk row t: the last s with q_off[s] <= t

@@ -83,3 +83,19 @@ def test_append_past_the_bound_writes_no_other_slot(most, long):
         want[most - 4:most] = r[:4]
         want[(pages - 2) * page + 18:(pages - 2) * page + 20] = r[new[0]:]
         assert torch.equal(slots, want)
+
+
+@pytest.mark.parametrize("new,most", [(4, 3), (8, 1), (40, 39), (200, 130)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 50), (False, 70)])
+def test_rows_past_the_bound_change_no_others(new, most, causal, window):
+    """Sequences of more rows than max_q are reported; the first max_q of them, and the other
+    sequences, have the positions and results that they have."""
+    c = Case([500, 3000, 90], [new, new, 1], heads=8, kvh=2, seed=new)
+    got = c.run(causal=causal, window=window, max_q=most)
+    torch.cuda.synchronize()
+    assert pc.workspace_status(got[3]) == 2
+    want, tol = c.want(causal=causal, window=window)
+    for first in (0, new, 2 * new):
+        rows = slice(first, first + (most if first < 2 * new else 1))
+        for i in range(2):
+            assert np.all(np.abs(got[i][rows].cpu().double().numpy() - want[i][rows]) <= tol[i][rows])

@@ -496,7 +496,9 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
  * row of page_table has room for or fewer.  Rows whose slot is negative, table
  * entries of n_pages or more that a call needs, lengths above max_kv and an
  * invalid q_off set the workspace status to 2; nothing is read or written out
- * of bounds.  Table entries past a sequence's length are not read.
+ * of bounds.  Table entries past a sequence's length are not read.  A call whose
+ * launches would hold 2^32 threads or more (as with 2^28 rows appended, or weights of
+ * 2^32 slots over all sequences and heads) returns PC_ERR_TOO_LARGE.
  * ------------------------------------------------------------------------ */
 typedef struct {
     void *k, *v;

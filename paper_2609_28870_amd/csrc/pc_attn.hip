@@ -672,7 +672,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
 #pragma unroll 8
                 for (uint32_t i = 0; i < rows; ++i) {
                     const float e = exp2_fast(x[i * a.score_stride] - stats[i]);   // NaN of a broken row: for what it sees
-                    sum += ((int32_t)j >= sees[i].x) & ((int32_t)j <= sees[i].y) ? e : 0.f;
+                    sum += (((int32_t)j >= sees[i].x) & ((int32_t)j <= sees[i].y)) ? e : 0.f;
                 }
                 w += sum;
             }
@@ -933,10 +933,39 @@ static size_t attn_carve(AttnArgs *a, const AttnPlan &p, char *ws, uint32_t n_se
     return c.off;
 }
 
+// Workgroups of the call's launches.
+struct AttnGrids {
+    uint64_t items;      // as many as there can be: the ones wanted, and one more for every tile of rows
+    uint32_t teams, row_blocks, key_blocks;   // of the join
+    uint64_t joins, weigh;                    // its two kinds of workgroups
+    uint64_t weights, sums;                   // of a chunk's weights
+};
+static AttnGrids attn_grids(const AttnPlan &p, const AttnArgs &a, uint64_t tiles) {
+    AttnGrids g;
+    g.items = a.target + tiles;
+    // few joins take several teams to a row (a decode batch: 8.7 us in 1,008 workgroups, 13 in
+    // 2,016); many are walked by at most 2048 workgroups, or one
+    // a tile (most of them find whole results and end)
+    const uint32_t all = 256 / (p.dim / 4);
+    g.teams = all;
+    while (g.teams > 1 && tiles * p.slot_rows * g.teams / all > 1024) g.teams /= 2;
+    g.row_blocks = (p.slot_rows * g.teams + all - 1) / all;
+    while (g.row_blocks > 1 && tiles * g.row_blocks > 2048) g.row_blocks = (g.row_blocks + 1) / 2;
+    g.key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
+    g.joins = tiles * g.row_blocks;
+    g.weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * g.key_blocks : 0;
+    const bool chunk_weights = a.weight_out && !p.few && a.max_kv;
+    g.sums = chunk_weights ? (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks : 0;
+    g.weights = g.sums * p.weight_parts;
+    return g;
+}
+static bool attn_fits(const AttnGrids &g, const AttnPlan &p) {
+    return launch_fits(g.items, p.few ? 256 : p.row_tile / 32 * WAVE) && launch_fits(g.joins + g.weigh, 256) && launch_fits(g.weights, 256);
+}
+
 template <class T, bool F8, int D, bool FULL>
-static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, hipStream_t st) {
-    // as many items as there can be: the ones wanted, and one more for every tile of rows
-    const dim3 items((unsigned)(a.target + tiles));
+static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
+    const dim3 items((unsigned)g.items);
     if (p.few) {
         if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
         else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, false>), items, dim3(256), 0, st, a);
@@ -946,33 +975,20 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, 
     } else {
         PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
     }
-    // few joins take several teams to a row (a decode batch: 8.7 us in 1,008 workgroups, 13 in
-    // 2,016); many are walked by at most 2048 workgroups, or one
-    // a tile (most of them find whole results and end)
-    constexpr uint32_t ALL = 256 / (D / 4);
-    uint32_t teams = ALL;
-    while (teams > 1 && tiles * p.slot_rows * teams / ALL > 1024) teams /= 2;
-    uint32_t row_blocks = (p.slot_rows * teams + ALL - 1) / ALL;
-    while (row_blocks > 1 && tiles * row_blocks > 2048) row_blocks = (row_blocks + 1) / 2;
-    const uint32_t key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
-    const uint64_t joins = tiles * row_blocks;
-    const uint64_t weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * key_blocks : 0;
-    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(joins + weigh)), dim3(256), 0, st, a, teams, (uint32_t)joins,
-              row_blocks, key_blocks);
-    if (a.weight_out && !p.few && a.max_kv) {
-        const uint64_t blocks = (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks;
-        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D, FULL>), dim3((unsigned)(blocks * p.weight_parts)), dim3(256), 0, st, a,
-                  p.key_blocks);
-        if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, p.key_blocks);
+    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(g.joins + g.weigh)), dim3(256), 0, st, a, g.teams, (uint32_t)g.joins,
+              g.row_blocks, g.key_blocks);
+    if (g.weights) {
+        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D, FULL>), dim3((unsigned)g.weights), dim3(256), 0, st, a, p.key_blocks);
+        if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)g.sums), dim3(256), 0, st, a, p.key_blocks);
     }
     return PC_OK;
 }
 template <class T, bool F8>
-static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, uint64_t tiles, hipStream_t st) {
+static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
     const bool full = a.kv.dim == p.dim;
-    if (p.dim == 64) return full ? attn_run<T, F8, 64, true>(a, p, tiles, st) : attn_run<T, F8, 64, false>(a, p, tiles, st);
-    if (p.dim == 128) return full ? attn_run<T, F8, 128, true>(a, p, tiles, st) : attn_run<T, F8, 128, false>(a, p, tiles, st);
-    return full ? attn_run<T, F8, 256, true>(a, p, tiles, st) : attn_run<T, F8, 256, false>(a, p, tiles, st);
+    if (p.dim == 64) return full ? attn_run<T, F8, 64, true>(a, p, g, st) : attn_run<T, F8, 64, false>(a, p, g, st);
+    if (p.dim == 128) return full ? attn_run<T, F8, 128, true>(a, p, g, st) : attn_run<T, F8, 128, false>(a, p, g, st);
+    return full ? attn_run<T, F8, 256, true>(a, p, g, st) : attn_run<T, F8, 256, false>(a, p, g, st);
 }
 
 }  // namespace pc
@@ -1014,7 +1030,6 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
         return PC_ERR_INVALID;
     const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim);
     const size_t need = attn_carve(&a, p, (char *)ws, n_seqs, n_rows, max_kv, n_heads, a.kv.n_kv, weight_out != nullptr);
-    if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     a.table = page_table;
     a.kv_len = kv_len;
@@ -1046,14 +1061,15 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.row_tile;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);
-    if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     // tiles of rows of every head, at most
     const uint64_t tiles = (p.few ? n_seqs : (uint64_t)n_rows * a.group / p.row_tile + n_seqs) * (uint64_t)a.kv.n_kv;
-    if (tiles * p.slot_rows + a.target > 0x7FFFFFFFu || (uint64_t)n_seqs * a.kv.n_kv * ((uint64_t)p.key_blocks + 1) * 16 > 0x7FFFFFFFu)
-        return PC_ERR_TOO_LARGE;
+    const AttnGrids g = attn_grids(p, a, tiles);
+    if (tiles * p.slot_rows + a.target > 0x7FFFFFFFu || !attn_fits(g, p)) return PC_ERR_TOO_LARGE;
+    if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
+    if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     const bool f8 = cache->dtype == PC_FP8_E4M3;
-    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, tiles, st) : attn_dim<Bf16, false>(a, p, tiles, st);
-    return f8 ? attn_dim<F16, true>(a, p, tiles, st) : attn_dim<F16, false>(a, p, tiles, st);
+    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, g, st) : attn_dim<Bf16, false>(a, p, g, st);
+    return f8 ? attn_dim<F16, true>(a, p, g, st) : attn_dim<F16, false>(a, p, g, st);
 }
 
 }  // extern "C"

@@ -27,6 +27,9 @@ struct KvView {
     FastDiv by_page;
 };
 
+// A launch holds fewer than 2^32 threads.
+inline bool launch_fits(uint64_t groups, uint32_t threads) { return groups < (1ull << 32) / threads; }
+
 pc_status kv_view(const pc_kv_cache *c, KvView *v);   // checks the descriptor
 size_t type_size(uint32_t dtype);                     // 0: no such type
 

@@ -245,12 +245,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     }
 }
 
+static bool append_many(uint32_t n_rows) { return n_rows >= APPEND_MANY; }
+static uint32_t append_groups(uint32_t n_rows) {
+    const uint32_t per = (append_many(n_rows) ? APPEND_ROWS : 1) * (256 / WAVE);
+    return 1 + (n_rows + per - 1) / per;
+}
+
 template <int MODE>
 static pc_status append_run(const AppendArgs &a, hipStream_t st) {
-    const bool many = a.n_rows >= APPEND_MANY;
-    const uint32_t per = (many ? APPEND_ROWS : 1) * (256 / WAVE);
-    const dim3 grid(1 + (a.n_rows + per - 1) / per);
-    if (many) PC_LAUNCH(K_KV_APPEND, append_kernel<MODE>, grid, dim3(256), 0, st, a);
+    const dim3 grid(append_groups(a.n_rows));
+    if (append_many(a.n_rows)) PC_LAUNCH(K_KV_APPEND, append_kernel<MODE>, grid, dim3(256), 0, st, a);
     else PC_LAUNCH(K_KV_APPEND, append_few_kernel<MODE>, grid, dim3(256), 0, st, a);
     return PC_OK;
 }
@@ -570,7 +574,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     if (ok != PC_OK) return ok;
     if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
     if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
-    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u) return PC_ERR_TOO_LARGE;
+    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u || !launch_fits(append_groups(n_rows), 256))
+        return PC_ERR_TOO_LARGE;
     if (max_kv > table_stride * a.kv.page) return PC_ERR_INVALID;
     if (!kv_len || !q_off || (max_kv && !page_table) || (n_rows && (!k || !v))) return PC_ERR_INVALID;
     if (((uint64_t)(uintptr_t)k | (uint64_t)(uintptr_t)v | k_stride_row * 2 | k_stride_head * 2 | v_stride_row * 2 |
@@ -622,7 +627,11 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     if (dst_table && (max_kv > table_stride * a.kv.page || budget > dst_stride * a.kv.page || (max_kv && !page_table)))
         return PC_ERR_INVALID;
     EvictSplit b;
-    if (!ws || ws_bytes < evict_carve((char *)ws, (uint64_t)n_seqs * a.kv.n_kv, max_kv, &a.status, &b)) return PC_ERR_WORKSPACE;
+    const uint32_t rows = n_seqs * a.kv.n_kv, groups = (budget < max_kv ? budget : max_kv) / MOVE_SLOTS + 1;
+    const size_t need = evict_carve((char *)ws, rows, max_kv, &a.status, &b);
+    if (!launch_fits(evict_split(max_kv) ? b.all : rows, SELECT_THREADS) || (dst_table && !launch_fits((uint64_t)rows * groups, 256)))
+        return PC_ERR_TOO_LARGE;
+    if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     a.table = page_table;
@@ -640,11 +649,7 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     a.new_len = new_len;
     a.weight_out = weight_out;
     a.by_piece = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
-    const unsigned rows = n_seqs * a.kv.n_kv;
-    const uint32_t groups = (budget < max_kv ? budget : max_kv) / MOVE_SLOTS + 1;
-    if (dst_table && (uint64_t)rows * groups > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
     if (evict_split(max_kv)) {
-        if (b.all > 0x7FFFFFFFu) return PC_ERR_TOO_LARGE;
         const dim3 grid((unsigned)b.all);
         PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<0>, grid, dim3(SELECT_THREADS), 0, st, a, b);
         PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<1>, grid, dim3(SELECT_THREADS), 0, st, a, b);

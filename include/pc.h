@@ -570,7 +570,8 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
  *   budget     1 ..; recent at most budget
  *   kept       uint32, [s][h] rows of `budget` entries: the slots kept, PC_NONE behind them
  *   weight_out float, the same layout: their weights, 0 behind them, or NULL
- *   new_len    uint32[n_seqs]: min(kv_len, budget)
+ *   new_len    uint32[n_seqs]: min(kv_len, budget).  kept, weight_out and new_len overlap neither
+ *              each other nor weight
  *   dst_table  uint32, [s] rows dst_stride apart of pages with room for `budget` slots, in the
  *              same cache, none of them a page of any of the call's sequences (shared
  *              prefix pages are never written); NULL: nothing is moved

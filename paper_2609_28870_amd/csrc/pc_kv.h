@@ -30,6 +30,12 @@ struct KvView {
 // A launch holds fewer than 2^32 threads.
 inline bool launch_fits(uint64_t groups, uint32_t threads) { return groups < (1ull << 32) / threads; }
 
+// whether two ranges of memory share a byte
+inline bool overlap(const void *a, uint64_t a_bytes, const void *b, uint64_t b_bytes) {
+    const uint64_t x = (uint64_t)(uintptr_t)a, y = (uint64_t)(uintptr_t)b;
+    return a_bytes && b_bytes && (x < y ? y - x < a_bytes : x - y < b_bytes);
+}
+
 pc_status kv_view(const pc_kv_cache *c, KvView *v);   // checks the descriptor
 size_t type_size(uint32_t dtype);                     // 0: no such type
 

@@ -405,8 +405,10 @@ __device__ __forceinline__ void place_kept(const EvictRow &e, const SlotKeys<N> 
         const uint64_t all = ballot(keep);
         if (keep) {
             const uint32_t r = at + mbcnt_acc(all, 0);
-            e.kept[r] = j0 + i * WAVE;
-            if (e.wout) e.wout[r] = slots.x[i];
+            if (r < e.need) {   // also where another stream changes the weights between two launches
+                e.kept[r] = j0 + i * WAVE;
+                if (e.wout) e.wout[r] = slots.x[i];
+            }
         }
         at += (uint32_t)__popcll(all);
     }
@@ -528,7 +530,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t g
     const uint32_t slots = min(MOVE_SLOTS, n - r0), pieces = slots * a.by_piece.d;
     for (uint32_t p = threadIdx.x; p < pieces; p += 256) {
         const uint32_t i = a.by_piece.div(p), c = p - i * a.by_piece.d, r = r0 + i;
-        const uint32_t j = a.kept[(uint64_t)row * a.budget + r];
+        const uint32_t j = min(a.kept[(uint64_t)row * a.budget + r], a.max_kv - 1);   // in bounds whatever else is written there
         const uint32_t js = a.kv.by_page.div(j), rs = a.kv.by_page.div(r);
         const uint32_t from = a.table[(uint64_t)s * a.table_stride + js], to = a.dst_table[(uint64_t)s * a.dst_stride + rs];
         if (from >= a.kv.n_pages || to >= a.kv.n_pages) {
@@ -555,6 +557,18 @@ static size_t evict_carve(char *ws, uint64_t rows, uint32_t max_kv, int32_t **st
         b->state = c.take<uint2>(2 * rows);
     }
     return c.off;
+}
+
+// whether a result shares memory with another, or with the weights that are still read
+static bool evict_overlaps(uint32_t rows, uint32_t n_seqs, uint32_t max_kv, const float *weight, uint64_t weight_stride, uint32_t budget,
+                           const uint32_t *kept, const float *weight_out, const uint32_t *new_len) {
+    const uint64_t out = (uint64_t)rows * budget * 4, in = rows && max_kv ? ((rows - 1) * weight_stride + max_kv) * 4 : 0;
+    const void *base[4] = {weight, kept, new_len, weight_out};
+    const uint64_t bytes[4] = {in, out, n_seqs * 4ull, weight_out ? out : 0};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j)
+            if (overlap(base[i], bytes[i], base[j], bytes[j])) return true;
+    return false;
 }
 
 }  // namespace pc
@@ -632,6 +646,7 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     if (!launch_fits(evict_split(max_kv) ? b.all : rows, SELECT_THREADS) || (dst_table && !launch_fits((uint64_t)rows * groups, 256)))
         return PC_ERR_TOO_LARGE;
     if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
+    if (evict_overlaps(rows, n_seqs, max_kv, weight, weight_stride, budget, kept, weight_out, new_len)) return PC_ERR_INVALID;
     const hipStream_t st = (hipStream_t)stream;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     a.table = page_table;

@@ -538,7 +538,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  *
  *   q, out     `dtype` PC_BF16 or PC_F16 (the cache the same or PC_FP8_E4M3), head e of
  *              row t at element t * stride_row + e * stride_head; pointers and
- *              strides in bytes multiples of 16
+ *              strides in bytes multiples of 16.  out may be q, with its strides, where no
+ *              weights are formed; else they do not overlap
  *   max_q      no sequence has more new rows (more set status 2, and what is past
  *              max_q may be left out); with max_q * group at most 32 the
  *              call takes the path for few rows

@@ -991,6 +991,35 @@ static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, const AttnGrids 
     return full ? attn_run<T, F8, 256, true>(a, p, g, st) : attn_run<T, F8, 256, false>(a, p, g, st);
 }
 
+// Two arrays [n_rows][n_heads] of runs of `width` bytes: whether they are one, and whether they
+// share memory.  In one range they are known not to if their strides agree and one lies in the
+// other's gaps, between its runs or between blocks of them.
+struct Entries {
+    const void *base;
+    uint64_t row, head;   // strides in bytes
+};
+static bool same_strides(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads) {
+    return (n_rows < 2 || x.row == y.row) && (n_heads < 2 || x.head == y.head);
+}
+static bool entries_overlap(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads, uint64_t width) {
+    if (!n_rows) return false;
+    auto extent = [&](const Entries &e) { return (n_rows - 1) * e.row + (n_heads - 1) * e.head + width; };
+    if (!overlap(x.base, extent(x), y.base, extent(y))) return false;
+    if (!same_strides(x, y, n_rows, n_heads)) return true;
+    const uint64_t apart = (uint64_t)(uintptr_t)y.base - (uint64_t)(uintptr_t)x.base, back = 0 - apart;
+    auto in_gaps = [&](uint64_t stride, uint64_t size) {   // of blocks of `size` bytes a stride apart
+        if (!stride) return false;
+        const uint64_t d = (int64_t)apart < 0 ? (stride - back % stride) % stride : apart % stride;
+        return d >= size && d + size <= stride;
+    };
+    if (n_rows < 2 && n_heads < 2) return true;
+    if (n_rows < 2 || n_heads < 2) return !in_gaps(n_rows < 2 ? x.head : x.row, width);
+    const bool by_row = x.head <= x.row;   // the heads of a row make a block, or the rows of a head
+    const uint64_t inner = by_row ? x.head : x.row, outer = by_row ? x.row : x.head, n = by_row ? n_heads : n_rows;
+    if (inner && outer % inner == 0 && in_gaps(inner, width)) return false;
+    return !in_gaps(outer, (n - 1) * inner + width);
+}
+
 }  // namespace pc
 
 extern "C" {
@@ -1066,6 +1095,10 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     const AttnGrids g = attn_grids(p, a, tiles);
     if (tiles * p.slot_rows + a.target > 0x7FFFFFFFu || !attn_fits(g, p)) return PC_ERR_TOO_LARGE;
     if (!ws || ws_bytes < need) return PC_ERR_WORKSPACE;
+    const Entries from{q, a.q_row, a.q_head}, to{out, a.o_row, a.o_head};
+    // in place, a row's query is read before its result is written, but for the weights' own pass
+    const bool in_place = q == out && same_strides(from, to, n_rows, n_heads) && !weight_out;
+    if (!in_place && entries_overlap(from, to, n_rows, n_heads, 2ull * a.kv.dim)) return PC_ERR_INVALID;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     const bool f8 = cache->dtype == PC_FP8_E4M3;
     if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, g, st) : attn_dim<Bf16, false>(a, p, g, st);

@@ -20,3 +20,23 @@ def test_eviction_results(L):   # noqa: F811
         refused(wout=FAKE + at)
     for at in (0, -8, weights - 4):
         refused(nl=FAKE + at)
+
+
+def test_attention_results(L):   # noqa: F811
+    """5 rows of 4 heads of 64 elements, 2 bytes each: runs of 128 bytes."""
+    def refused(out, **kw):
+        assert attn(L, out=out, **kw) == -1
+    for at in (16, 128, 512, 4 * 512 + 496, -16, -512, 16 - 2560):
+        refused(FAKE + at)                                        # dense, at another place
+    refused(FAKE, wout=FAKE + 0x10000, wstride=64)                # in place, with weights
+    refused(FAKE, outr=512)                                       # in place, other strides
+    refused(FAKE, outh=128, outr=512)
+    wide = dict(qr=512, outr=512)                                 # rows of 1,024 bytes, half of them used
+    for at in (0, 16, 496, 528, -16, 1024 + 16):
+        refused(FAKE + at, wout=FAKE + 0x10000, wstride=64, **wide)
+    heads_apart = dict(qh=128, outh=128, qr=512, outr=512)        # runs with gaps of their own length
+    for at in (16, 112, 144, 256, -16):
+        refused(FAKE + at, **heads_apart)
+    heads_first = dict(qr=128, outr=128, qh=640, outh=640)        # [head][row], runs with gaps
+    for at in (16, 112, 144, 256, -16):
+        refused(FAKE + at, **heads_first)

@@ -99,3 +99,32 @@ def test_rows_past_the_bound_change_no_others(new, most, causal, window):
         rows = slice(first, first + (most if first < 2 * new else 1))
         for i in range(2):
             assert np.all(np.abs(got[i][rows].cpu().double().numpy() - want[i][rows]) <= tol[i][rows])
+
+
+@pytest.mark.parametrize("new", [1, 5, 40])
+@pytest.mark.parametrize("kv", [200, 3000])
+def test_results_in_place_and_between_queries(new, kv):
+    """out over q itself, and in the gaps of q's rows, heads and [head, row] blocks."""
+    c = Case([kv, 90], [new, new], heads=8, kvh=2, seed=kv + new)
+    want = [x.clone() for x in c.run()[:2]]
+    q, (rows, heads, dim) = c.q.clone(), c.q.shape
+    empty = lambda *shape: torch.zeros(shape, dtype=c.dtype, device="cuda")   # noqa: E731
+    pairs = [(x, x) for x in (q.clone(),)]
+    x = empty(rows, 2 * heads, dim)
+    pairs.append((x[:, :heads], x[:, heads:]))
+    x = empty(rows, 2 * heads, dim)
+    pairs.append((x[:, heads:], x[:, :heads]))
+    x = empty(rows, heads, 2 * dim)
+    pairs.append((x[..., :dim], x[..., dim:]))
+    x = empty(heads, rows, 2 * dim)
+    pairs.append((x[..., :dim].transpose(0, 1), x[..., dim:].transpose(0, 1)))
+    x = empty(heads, 2 * rows, dim)
+    pairs.append((x[:, :rows].transpose(0, 1), x[:, rows:].transpose(0, 1)))
+    for src, dst in pairs:
+        src.copy_(q)
+        c.q = src
+        got = c.run(out=dst)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    c.q = q
+    with pytest.raises(pc.PcError):
+        c.run(out=c.q, weight_out=torch.zeros((2, 2, c.cols * 16), device="cuda"))

@@ -510,6 +510,7 @@ def belady(nxt: torch.Tensor, caps: torch.Tensor, depth: Optional[torch.Tensor] 
 # ------------------------------------------------------------- paged cache
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}   # PC_BF16, PC_F16, PC_FP8_E4M3
+_INTS = (torch.int32, torch.uint32)
 _MAX_KV = 0x7FFF0000
 
 
@@ -528,13 +529,13 @@ def _table(t: torch.Tensor, what: str, rows: int):
     if not t.is_cuda:
         raise PcError("expected a GPU tensor")
     shape, stride = t.shape, t.stride()
-    if t.element_size() != 4 or len(shape) != 2 or shape[0] != rows or (shape[1] > 1 and stride[1] != 1):
-        raise PcError("%s: expected [%d, columns] of 32 bits, columns contiguous" % (what, rows))
+    if t.dtype not in _INTS or len(shape) != 2 or shape[0] != rows or (shape[1] > 1 and stride[1] != 1):
+        raise PcError("%s: expected [%d, columns] of 32-bit integers, columns contiguous" % (what, rows))
     return t.data_ptr(), stride[0] if rows > 1 else shape[1]
 
 
 def _index(t: torch.Tensor, what: str, n: int):
-    if t.dtype not in (torch.int32, torch.uint32) or t.shape != (n,):
+    if t.dtype not in _INTS or t.shape != (n,):
         raise PcError("%s: expected [%d] of 32-bit integers" % (what, n))
     return _ptr(t)
 

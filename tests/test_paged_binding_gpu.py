@@ -1,0 +1,47 @@
+"""The binding of the operators over a paged cache refuses what it would misread or lose."""
+import pytest
+import torch
+
+from paper_2609_28870_amd import pc
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    yield
+    torch.cuda.synchronize()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def calls():
+    """(call, arguments that it takes) of the three operators: two sequences of 20 and 9 slots, 4 and 2 of them new."""
+    k, v = (torch.randn((6, 2, 16, 32), device="cuda").to(BF16) for _ in range(2))
+    seqs = dict(cache=pc.PagedCache(k, v), page_table=i32([[0, 1], [2, 3]]), kv_len=i32([20, 9]))
+    rows = [torch.randn((6, n, 32), device="cuda").to(BF16) for n in (4, 2, 2)]
+    return dict(append=(pc.kv_append, dict(seqs, q_off=i32([0, 4, 6]), k=rows[1], v=rows[2])),
+                attn=(pc.attn_paged, dict(seqs, q_off=i32([0, 4, 6]), q=rows[0], max_q=4)),
+                evict=(pc.kv_evict, dict(seqs, weight=torch.rand((2, 2, 32), device="cuda"), budget=8, recent=2,
+                                         dst_table=i32([[4], [5]]))))
+
+
+def refused(name, **kw):
+    call, args = calls()[name]
+    call(**args)
+    with pytest.raises(pc.PcError):
+        call(**dict(args, **kw))
+    torch.cuda.synchronize()
+
+
+def test_tables_of_other_types():
+    for name in ("append", "attn", "evict"):
+        refused(name, page_table=torch.zeros((2, 2), device="cuda"))
+    refused("evict", dst_table=torch.zeros((2, 1), device="cuda"))
+    call, args = calls()["attn"]
+    want = call(**args)[0]
+    assert torch.equal(call(**dict(args, page_table=args["page_table"].view(torch.uint32)))[0], want)

@@ -692,10 +692,11 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
         out = {"kept": weight.new_empty(shape, dtype=torch.int32), "weight": weight.new_empty(shape),
                "new_len": kv_len.new_empty((n_seqs,))}
     else:
-        for name in ("kept", "weight"):
-            x = out.get(name)
-            if (x is None and name == "kept") or (x is not None and (x.shape != shape or x.element_size() != 4)):
-                raise PcError("%s: expected [sequences, kv heads, budget] of 32 bits" % name)
+        kept, w = out.get("kept"), out.get("weight")
+        if kept is None or kept.shape != shape or kept.dtype not in _INTS:
+            raise PcError("kept: expected [sequences, kv heads, budget] of 32-bit integers")
+        if w is not None and (w.shape != shape or w.dtype != torch.float32):
+            raise PcError("weight: expected [sequences, kv heads, budget] float32")
     if ws is None:
         ws = _scratch(L.pc_kv_evict_ws(n_seqs, heads, max_kv), weight)
     check(L.pc_kv_evict(cache._at, table, stride, _index(kv_len, "kv_len", n_seqs), n_seqs, max_kv, _ptr(weight),

@@ -45,3 +45,15 @@ def test_tables_of_other_types():
     call, args = calls()["attn"]
     want = call(**args)[0]
     assert torch.equal(call(**dict(args, page_table=args["page_table"].view(torch.uint32)))[0], want)
+
+
+def test_eviction_results_of_other_types():
+    out = dict(kept=torch.empty((2, 2, 8), dtype=torch.int32, device="cuda"), weight=torch.empty((2, 2, 8), device="cuda"),
+               new_len=i32([0, 0]))
+    refused("evict", out=dict(out, kept=torch.empty((2, 2, 8), device="cuda")))
+    refused("evict", out=dict(out, weight=torch.empty((2, 2, 8), dtype=torch.int32, device="cuda")))
+    refused("evict", out=dict(out, kept=None))
+    refused("evict", out=dict(out, new_len=torch.empty(2, device="cuda")))
+    call, args = calls()["evict"]
+    assert call(**dict(args, out=dict(out, weight=None)))["weight"] is None
+    assert call(**dict(args, out=dict(out)))["new_len"].tolist() == [8, 8]

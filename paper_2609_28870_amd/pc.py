@@ -550,6 +550,12 @@ def _rows(t: torch.Tensor, what: str, shape):
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[2], stride[1] if shape[1] > 1 else shape[2]
 
 
+def _no_gradient():
+    """There is no backward pass: what autograd would follow is refused rather than cut off."""
+    if torch.is_grad_enabled():
+        raise PcError("no backward pass: call under torch.no_grad() or detach what requires a gradient")
+
+
 def _room(page_table: torch.Tensor, cache, max_kv: Optional[int]) -> int:
     room = page_table.shape[1] * cache.page_size
     if max_kv is None:
@@ -563,7 +569,9 @@ class PagedCache:
     """A paged cache of KV blocks (``pc_kv_cache``) over two tensors [page, head,
     slot, head_dim] of one type and one set of strides, head_dim contiguous: pages
     kept as [page, slot, head, head_dim] go in as ``x.transpose(1, 2)``.  bfloat16,
-    float16, or float8_e4m3fn with ``k_scale`` and ``v_scale`` (float32, one per head)."""
+    float16, or float8_e4m3fn with ``k_scale`` and ``v_scale`` (float32, one per head).
+    The calls on it have no backward pass and refuse tensors that require a gradient
+    (outside of ``torch.no_grad()``)."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
@@ -580,6 +588,8 @@ class PagedCache:
             if x is not None and (x.dtype != torch.float32 or x.shape != shape[1:2]):
                 raise PcError("expected one float32 scale per head")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._grad = k.requires_grad or v.requires_grad or (
+            k_scale is not None and (k_scale.requires_grad or v_scale.requires_grad))
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
         if 1 in shape:   # the stride of a dimension of one is anything
             stride = [s if n > 1 else self.head_dim for s, n in zip(stride, shape)]
@@ -593,6 +603,8 @@ def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor,
     """pc_kv_append: rows q_off[s] .. q_off[s + 1] - 1 of ``k`` and ``v`` ([rows, head,
     head_dim]) into the last slots of the kv_len[s] of sequence s."""
     L = lib()
+    if k.requires_grad or v.requires_grad or cache._grad:
+        _no_gradient()
     n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
     max_kv = _room(page_table, cache, max_kv)
@@ -622,6 +634,8 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_
     ([sequence, kv head, max_kv] float32) are formed when ``weight`` or ``weight_out``
     is given."""
     L = lib()
+    if q.requires_grad or cache._grad or (weight is not None and weight.requires_grad):
+        _no_gradient()
     n_seqs = kv_len.shape[0]
     table, stride = _table(page_table, "page_table", n_seqs)
     max_kv = _room(page_table, cache, max_kv)
@@ -670,6 +684,8 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
     Their keys and values move to the pages of ``dst_table`` when it is given.  Returns
     {"kept" (int32, -1 behind the last), "weight", "new_len", "ws"}."""
     L = lib()
+    if weight.requires_grad or cache._grad:
+        _no_gradient()
     n_seqs = kv_len.shape[0]
     if budget < 1 or not 0 <= recent <= budget:
         raise PcError("expected a budget of at least 1, and 0 <= recent <= budget")

@@ -57,3 +57,19 @@ def test_eviction_results_of_other_types():
     call, args = calls()["evict"]
     assert call(**dict(args, out=dict(out, weight=None)))["weight"] is None
     assert call(**dict(args, out=dict(out)))["new_len"].tolist() == [8, 8]
+
+
+def test_what_requires_a_gradient():
+    """There is no backward pass: a gradient that would be lost is refused, outside of no_grad."""
+    wants = {"append": ("k", "v"), "attn": ("q", "weight"), "evict": ("weight",)}
+    for name, keys in wants.items():
+        for key in keys:
+            call, args = calls()[name]
+            x = args.get(key)
+            x = torch.rand((2, 2, 32), device="cuda") if x is None else x
+            refused(name, **{key: x.clone().requires_grad_()})
+            with torch.no_grad():
+                call(**dict(args, **{key: x.requires_grad_()}))
+    cache = calls()["attn"][1]["cache"]
+    k = cache.k.clone().requires_grad_()
+    refused("attn", cache=pc.PagedCache(k, cache.v))

@@ -560,8 +560,8 @@ def _room(page_table: torch.Tensor, cache, max_kv: Optional[int]) -> int:
     room = page_table.shape[1] * cache.page_size
     if max_kv is None:
         return min(room, _MAX_KV)
-    if not 0 <= max_kv <= room:
-        raise PcError("max_kv: the page table has fewer slots")
+    if not 0 <= max_kv <= min(room, _MAX_KV):
+        raise PcError("max_kv: the page table has fewer slots, or more than 2^31 - 2^16")
     return max_kv
 
 
@@ -640,8 +640,8 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_
     table, stride = _table(page_table, "page_table", n_seqs)
     max_kv = _room(page_table, cache, max_kv)
     dtype, shape = _DTYPES.get(q.dtype), q.shape
-    if window < 0 or max_q < 0:
-        raise PcError("window and max_q: expected at least 0")
+    if not 0 <= window <= NONE or not 0 <= max_q <= NONE:
+        raise PcError("window and max_q: expected at least 0 and below 2^32")
     if len(shape) != 3 or dtype is None or shape[2] != cache.head_dim:
         raise PcError("expected q as [rows, heads, %d] of bfloat16 or float16" % cache.head_dim)
     n_rows, n_heads, dim = shape
@@ -687,8 +687,8 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
     if weight.requires_grad or cache._grad:
         _no_gradient()
     n_seqs = kv_len.shape[0]
-    if budget < 1 or not 0 <= recent <= budget:
-        raise PcError("expected a budget of at least 1, and 0 <= recent <= budget")
+    if not 1 <= budget <= _MAX_KV or not 0 <= recent <= budget:
+        raise PcError("expected a budget of 1 to 2^31 - 2^16, and 0 <= recent <= budget")
     table, stride = _table(page_table, "page_table", n_seqs)
     heads = cache.n_kv_heads
     if weight.dtype != torch.float32 or len(weight.shape) != 3 or weight.shape[:2] != (n_seqs, heads):

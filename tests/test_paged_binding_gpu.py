@@ -73,3 +73,23 @@ def test_what_requires_a_gradient():
     cache = calls()["attn"][1]["cache"]
     k = cache.k.clone().requires_grad_()
     refused("attn", cache=pc.PagedCache(k, cache.v))
+
+
+def test_bounds_above_32_bits():
+    """Sizes that would lose their upper bits on the way."""
+    top = 1 << 32
+    for kw in (dict(max_q=top + 4), dict(window=top + 3)):
+        refused("attn", **kw)
+    refused("evict", budget=top + 8)
+    refused("evict", budget=top + 8, dst_table=None)
+    # room for more than 2^32 slots, a page many times over
+    table = torch.zeros((1, 65600), dtype=torch.int32, device="cuda")
+    k = torch.zeros((1, 1, 65536, 16), dtype=BF16, device="cuda")
+    cache, x = pc.PagedCache(k, k.clone()), torch.ones((1, 1, 16), dtype=BF16, device="cuda")
+    for max_kv in (top + 5, top + 33):
+        with pytest.raises(pc.PcError):
+            pc.kv_append(cache, table, i32([33]), i32([0, 1]), x, x, max_kv=max_kv)
+        with pytest.raises(pc.PcError):
+            pc.attn_paged(x, cache, table, i32([33]), i32([0, 1]), 1, max_kv=max_kv)
+    assert pc.workspace_status(pc.kv_append(cache, table, i32([33]), i32([0, 1]), x, x)) == 0
+    assert bool((k[0, 0, 32] == 1).all()) and not bool(k[0, 0, :32].any())

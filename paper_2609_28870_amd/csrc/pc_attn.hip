@@ -886,14 +886,19 @@ constexpr uint32_t ROWS_ITEMS = 1024;
 constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_WIDE = 256, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
 constexpr uint32_t WIDE_ROWS = 1024, WIDE_KEYS = 8192;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
+// Few rows with weights: up to 2^30 scores (rows times room) are kept, a workspace of 4 GiB.  Above
+// that the weights take the chunks' second pass over the keys, which is slower but needs
+// no room (32 sequences of 32,768 keys, 8 heads: 32 rows a head 1,468 us with 1 GB of scores and
+// 1,508 without; uneven lengths 387 and 537; 64 of 4 heads with 8 rows each 1,055 and 1,466).
+constexpr uint64_t SCORES_MOST = 1ull << 30;
 constexpr uint32_t WEIGHT_ITEMS = 4096;   // with 1024, two rounds of the chip, uneven ends took a quarter of the time
 
 struct AttnPlan {
-    bool few, wide;
+    bool few, wide, scores;
     uint32_t row_tile, dim, items, slots, slot_rows, weight_parts, key_blocks;
     uint64_t score_stride;
 };
-static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim) {
+static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim, bool weights) {
     AttnPlan p;
     const uint32_t group = n_heads / n_kv;
     p.few = (uint64_t)max_q * group <= ROWS_MOST;
@@ -905,6 +910,8 @@ static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint
     p.slots = 2 * p.items;
     p.slot_rows = p.few ? (max_q ? max_q : 1) * group : p.row_tile;
     p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
+    const uint64_t score_rows = (uint64_t)n_seqs * n_kv * p.slot_rows;
+    p.scores = weights && p.few && score_rows <= SCORES_MOST && score_rows * p.score_stride <= SCORES_MOST;
     p.key_blocks = (uint32_t)(((uint64_t)max_kv + WEIGHT_KEYS - 1) / WEIGHT_KEYS);
     const uint64_t blocks = (uint64_t)n_seqs * n_kv * (p.key_blocks ? p.key_blocks : 1);
     const uint64_t tiles = ((uint64_t)max_q * group + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
@@ -923,7 +930,7 @@ static size_t attn_carve(AttnArgs *a, const AttnPlan &p, char *ws, uint32_t n_se
     a->scores = a->weight_part = nullptr;
     if (weights) {
         a->lse2 = c.take<float>((size_t)n_rows * n_heads);
-        if (p.few) a->scores = c.take<float>((size_t)n_seqs * n_kv * p.slot_rows * p.score_stride);
+        if (p.scores) a->scores = c.take<float>((size_t)n_seqs * n_kv * p.slot_rows * p.score_stride);
         else if (p.weight_parts > 1) a->weight_part = c.take<float>((size_t)p.weight_parts * n_seqs * n_kv * max_kv);
     }
     a->slots = p.slots;
@@ -938,7 +945,7 @@ struct AttnGrids {
     uint64_t items;      // as many as there can be: the ones wanted, and one more for every tile of rows
     uint32_t teams, row_blocks, key_blocks;   // of the join
     uint64_t joins, weigh;                    // its two kinds of workgroups
-    uint64_t weights, sums;                   // of a chunk's weights
+    uint64_t weights, sums;                   // of the weights' second pass
 };
 static AttnGrids attn_grids(const AttnPlan &p, const AttnArgs &a, uint64_t tiles) {
     AttnGrids g;
@@ -953,9 +960,8 @@ static AttnGrids attn_grids(const AttnPlan &p, const AttnArgs &a, uint64_t tiles
     while (g.row_blocks > 1 && tiles * g.row_blocks > 2048) g.row_blocks = (g.row_blocks + 1) / 2;
     g.key_blocks = (uint32_t)(((uint64_t)a.max_kv + WEIGH_KEYS - 1) / WEIGH_KEYS);
     g.joins = tiles * g.row_blocks;
-    g.weigh = p.few && a.weight_out ? (uint64_t)a.n_seqs * a.kv.n_kv * g.key_blocks : 0;
-    const bool chunk_weights = a.weight_out && !p.few && a.max_kv;
-    g.sums = chunk_weights ? (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks : 0;
+    g.weigh = p.scores ? (uint64_t)a.n_seqs * a.kv.n_kv * g.key_blocks : 0;
+    g.sums = a.weight_out && !p.scores ? (uint64_t)a.n_seqs * a.kv.n_kv * p.key_blocks : 0;
     g.weights = g.sums * p.weight_parts;
     return g;
 }
@@ -967,7 +973,7 @@ template <class T, bool F8, int D, bool FULL>
 static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
     const dim3 items((unsigned)g.items);
     if (p.few) {
-        if (a.weight_out) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
+        if (p.scores) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
         else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, false>), items, dim3(256), 0, st, a);
     } else if (p.wide) {
         constexpr int W = D == 128 ? CHUNK_WAVES_WIDE : CHUNK_WAVES;
@@ -1029,7 +1035,7 @@ size_t pc_attn_paged_ws(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32
     using namespace pc;
     if (!n_heads || !n_kv_heads || n_heads % n_kv_heads) return WS_HEADER;
     AttnArgs a;
-    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim);
+    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, with_weight != 0);
     return attn_carve(&a, p, nullptr, n_seqs, n_rows, max_kv, n_heads, n_kv_heads, with_weight != 0);
 }
 
@@ -1057,7 +1063,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     if (((uint64_t)(uintptr_t)q | (uint64_t)(uintptr_t)out | q_stride_row * 2 | q_stride_head * 2 | out_stride_row * 2 |
          out_stride_head * 2) % 16)
         return PC_ERR_INVALID;
-    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim);
+    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim, weight_out != nullptr);
     const size_t need = attn_carve(&a, p, (char *)ws, n_seqs, n_rows, max_kv, n_heads, a.kv.n_kv, weight_out != nullptr);
     const hipStream_t st = (hipStream_t)stream;
     a.table = page_table;

@@ -33,3 +33,14 @@ def test_eviction(L):   # noqa: F811
     assert evict(L, n_seqs=(1 << 15) - 1, ws=None, **dict(long, dst=None)) == -3
     assert evict(L, n_seqs=512, **long) == -2
     assert evict(L, n_seqs=511, ws=None, **long) == -3
+
+
+def test_workspace_of_scores(L):   # noqa: F811
+    """Few rows with weights: what holds their scores is bounded, whatever the room for slots is."""
+    parts = L.pc_attn_paged_ws(96, 384, 4, 131072, 64, 8, 128, 0)
+    assert L.pc_attn_paged_ws(96, 384, 4, 131072, 64, 8, 128, 1) < parts + (1 << 20)
+    for max_kv in (1 << 10, 1 << 15, 1 << 16, 1 << 17, 1 << 20, 0x7FFF0000):
+        assert L.pc_attn_paged_ws(64, 256, 4, max_kv, 64, 8, 128, 1) <= parts + (4 << 30) + (1 << 20)
+    most = (1 << 30) // (64 * 32 * 8)
+    assert L.pc_attn_paged_ws(64, 256, 4, most, 64, 8, 128, 1) >= 4 << 30
+    assert L.pc_attn_paged_ws(64, 256, 4, most + 1, 64, 8, 128, 1) < 1 << 28

@@ -524,8 +524,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
                        size_t ws_bytes, void *stream);
 
 /* Attention of new tokens over the cache (which holds them already).
- *     slots a row at position x sees: j < kv_len[s], j <= x if PC_ATTN_CAUSAL,
- *                                     j > x - window if window > 0
+ *     slots a row in slot x sees: j < kv_len[s], j <= x if PC_ATTN_CAUSAL,
+ *                                 j > x - window if window > 0
  *     s_j = scale * <q, k_j>    lse = log sum_j exp(s_j)
  *     out = sum_j exp(s_j - lse) v_j
  *     weight_out[s][h][j] = weight[s][h][j] + sum over the chunk's rows and the
@@ -569,6 +569,10 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
  * The last min(recent, that) stay; the rest of the places go to the largest
  * weights (equal ones: the lowest slot first; NaN is above infinity), in slot
  * order.  Kept slot number r moves to slot r of the destination table's row.
+ *
+ * The slots of a cut sequence are numbered anew, and pc_attn_paged takes slots for
+ * positions: causal order holds, but a window then spans that many kept tokens, not
+ * tokens of the text, and heads may keep different ones.
  *
  *   weight     as in pc_attn_paged
  *   budget     1 ..; recent at most budget

@@ -681,7 +681,8 @@ def kv_evict(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, 
              out: Optional[dict] = None, ws: Optional[torch.Tensor] = None):
     """pc_kv_evict: per (sequence, head) the last ``recent`` slots and those of the
     largest ``weight`` ([sequence, kv head, at least max_kv] float32), ``budget`` in all, in slot order.
-    Their keys and values move to the pages of ``dst_table`` when it is given.  Returns
+    Their keys and values move to the pages of ``dst_table`` when it is given; slots are
+    numbered anew, and a later ``attn_paged(window=...)`` counts kept slots.  Returns
     {"kept" (int32, -1 behind the last), "weight", "new_len", "ws"}."""
     L = lib()
     if weight.requires_grad or cache._grad:

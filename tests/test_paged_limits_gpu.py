@@ -147,3 +147,31 @@ def test_weights_of_few_rows_with_room_for_many_slots(cache, window):
     got = c.run(window=window, weight_out=c.weight)[2].clone()      # in place
     c.weight = base
     c.check(got=(None, None, got, below[3]), window=window)
+
+
+@pytest.mark.parametrize("dim", [144, 256])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, FP8), (F16, FP8)], ids=["bf16", "f16", "bf16-fp8", "f16-fp8"])
+def test_cut_sequences_of_wide_heads(dim, new, dtype, cache):
+    """Parts and joins of 256 dimensions, and more than 64 groups of 16 slots in a range."""
+    for heads, kvh, page in ((8, 1, 16), (4, 2, 24)):
+        c = Case([5000, 300], [new, new], heads=heads, kvh=kvh, dim=dim, page=page, dtype=dtype, cache=cache, seed=dim + new,
+                 weights=True)
+        c.check()
+        c.check(window=1700)
+
+
+@pytest.mark.parametrize("n", [65, 150])
+@pytest.mark.parametrize("new", [1, 12])
+@pytest.mark.parametrize("page", [16, 10])
+def test_cut_sequences_among_many(n, new, page):
+    """More sequences than lanes of a wave, with cut ones before and behind the 64th."""
+    r = np.random.default_rng(n + new)
+    kv = r.integers(0, 90, n)
+    for s in (0, 5, 63, 64, n - 1):
+        kv[s] = r.integers(2000, 4000)
+    m = np.minimum(r.integers(0, new + 1, n), kv)
+    m[[0, 5, 63, 64, n - 1]] = new
+    c = Case(kv, m, heads=8, kvh=2, dim=32, page=page, seed=n + new, weights=True)
+    c.check()
+    c.check(window=900)

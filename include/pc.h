@@ -550,8 +550,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  *              entries are written, 0 from kv_len on.
  *   n_heads    a multiple of n_kv_heads; scale finite
  * With few rows and weights the workspace holds the scores, 4 bytes a new row, query head and
- * slot of max_kv (n_seqs * max_q * n_heads * max_kv in all), up to 4 GiB of them; above
- * that they are formed twice and take none.
+ * slot of max_kv (n_seqs * max_q * n_heads * max_kv in all), or 4 GiB if they are more;
+ * then they are formed twice instead.
  * Scores, statistics and sums are in 32 bits; exp(s_j - max) is rounded to `dtype`
  * for its product with v.  Results do not depend on timing (no atomics). */
 size_t pc_attn_paged_ws(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32_t max_kv, uint32_t n_heads,

@@ -887,8 +887,8 @@ constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_WIDE = 256, CHUNK_ITEMS_RAGGED
 constexpr uint32_t WIDE_ROWS = 1024, WIDE_KEYS = 8192;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
 // Few rows with weights: up to 2^30 scores (rows times room) are kept, a workspace of 4 GiB.  Above
-// that the weights take the chunks' second pass over the keys, which is slower but needs
-// no room (32 sequences of 32,768 keys, 8 heads: 32 rows a head 1,468 us with 1 GB of scores and
+// that the weights take the chunks' second pass over the keys, which is slower but keeps
+// none (32 sequences of 32,768 keys, 8 heads: 32 rows a head 1,468 us with 1 GB of scores and
 // 1,508 without; uneven lengths 387 and 537; 64 of 4 heads with 8 rows each 1,055 and 1,466).
 constexpr uint64_t SCORES_MOST = 1ull << 30;
 constexpr uint32_t WEIGHT_ITEMS = 4096;   // with 1024, two rounds of the chip, uneven ends took a quarter of the time
@@ -896,7 +896,7 @@ constexpr uint32_t WEIGHT_ITEMS = 4096;   // with 1024, two rounds of the chip, 
 struct AttnPlan {
     bool few, wide, scores;
     uint32_t row_tile, dim, items, slots, slot_rows, weight_parts, key_blocks;
-    uint64_t score_stride;
+    uint64_t score_stride, score_room;   // scores of a row, and of the call that the workspace holds
 };
 static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim, bool weights) {
     AttnPlan p;
@@ -910,8 +910,11 @@ static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint
     p.slots = 2 * p.items;
     p.slot_rows = p.few ? (max_q ? max_q : 1) * group : p.row_tile;
     p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
-    const uint64_t score_rows = (uint64_t)n_seqs * n_kv * p.slot_rows;
-    p.scores = weights && p.few && score_rows <= SCORES_MOST && score_rows * p.score_stride <= SCORES_MOST;
+    // a workspace for some bounds holds out for lower ones, so above SCORES_MOST it does not shrink
+    const uint64_t score_rows = p.few && weights ? (uint64_t)n_seqs * n_kv * p.slot_rows : 0;
+    const bool fit = score_rows <= SCORES_MOST && score_rows * p.score_stride <= SCORES_MOST;
+    p.scores = p.few && weights && fit;
+    p.score_room = fit ? score_rows * p.score_stride : SCORES_MOST;
     p.key_blocks = (uint32_t)(((uint64_t)max_kv + WEIGHT_KEYS - 1) / WEIGHT_KEYS);
     const uint64_t blocks = (uint64_t)n_seqs * n_kv * (p.key_blocks ? p.key_blocks : 1);
     const uint64_t tiles = ((uint64_t)max_q * group + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
@@ -930,7 +933,7 @@ static size_t attn_carve(AttnArgs *a, const AttnPlan &p, char *ws, uint32_t n_se
     a->scores = a->weight_part = nullptr;
     if (weights) {
         a->lse2 = c.take<float>((size_t)n_rows * n_heads);
-        if (p.scores) a->scores = c.take<float>((size_t)n_seqs * n_kv * p.slot_rows * p.score_stride);
+        if (p.few) a->scores = c.take<float>(p.score_room);
         else if (p.weight_parts > 1) a->weight_part = c.take<float>((size_t)p.weight_parts * n_seqs * n_kv * max_kv);
     }
     a->slots = p.slots;

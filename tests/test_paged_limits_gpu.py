@@ -133,13 +133,12 @@ def test_results_in_place_and_between_queries(new, kv):
 @pytest.mark.parametrize("cache", ["same", "fp8"])
 @pytest.mark.parametrize("window", [0, 300])
 def test_weights_of_few_rows_with_room_for_many_slots(cache, window):
-    """Above 2^30 scores of room the workspace holds none, and results are what they are below."""
+    """Above 2^30 scores of room none are kept, and results are what they are below."""
     c = Case([700, 3000, 0, 65] + [20] * 60, [4, 1, 0, 3] + [2] * 60, heads=64, kvh=8, dim=64, page=64,
              cache=FP8 if cache == "fp8" else None, weights=True, seed=11, cols=1 + (1 << 30) // (64 * 8 * 32 * 64))
     got = c.run(window=window)
-    assert got[3].numel() < 1 << 28
     c.check(got=got, window=window)
-    below = c.run(window=window, max_kv=3008)
+    below = c.run(window=window, max_kv=3008, ws=got[3])
     torch.cuda.synchronize()
     for x, y in zip(got[:2], below[:2]):
         assert torch.equal(x, y)

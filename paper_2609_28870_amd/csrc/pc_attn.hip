@@ -877,14 +877,19 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(AttnArgs a, uint32_t ke
 
 constexpr uint32_t ROWS_MOST = 32;           // rows of the path for few rows
 constexpr uint32_t ROWS_ITEMS = 1024;
-// Chunks: one round of the chip, 512 workgroups of four waves, or 256 of eight.  The wide
-// ones take few sequences of many rows over long caches in heads of 65 to 128 dimensions
-// (2,048 tokens over 32,768: 1,050 us, 1,141 narrow; 128 over 32,768: 96, 99; but 2,048 over
-// 4,096: 148, 140, and 12 ragged chunks: 230, 195).  Of several sequences, uneven
-// lengths leave gaps that smaller items fill (12 ragged chunks: 227 to 197 us), which
-// costs a join where there was none (one chunk of 2,048 over 32,768: 18 us).
-constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_WIDE = 256, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 4;
-constexpr uint32_t WIDE_ROWS = 1024, WIDE_KEYS = 8192;
+// Chunks: one round of the chip, 512 workgroups of four waves, or 256 of eight.  The wide ones take
+// one to three sequences of at least 2,048 rows (tokens times heads of a group) for each of them, with
+// room for 8,192 slots, in heads of 65 to 128 dimensions: 6% faster in the mean of 122 such shapes (all
+// types, 1 to 12 key/value heads, 8,192 and 32,768 keys; 2,048 tokens over 32,768: 1,068 us, 1,177
+// narrow), 22% slower at worst.  The 230 shapes measured below those bounds were 2% slower, 46% at
+// worst (three sequences of 1,024 rows); a cache that does not use its room, 4%.
+// Smaller items, those of cut sequences first, fill the gaps that uneven lengths leave: of twelve
+// sequences on whose rows are under 7/8 of what max_q allows 640 items are wanted (12 sequences: 1%
+// slower in the mean of 38 shapes, of which they take 0.82 to 1.17 of the time; 14 to 48: 3% faster in the
+// mean of 150).  Of fewer sequences they took 4% more time, and of even ones up to 56%: each
+// is cut into one part more than the round holds.
+constexpr uint32_t CHUNK_ITEMS = 512, CHUNK_ITEMS_WIDE = 256, CHUNK_ITEMS_RAGGED = 640, RAGGED_SEQS = 12;
+constexpr uint32_t WIDE_SEQS = 3, WIDE_ROWS = 2048, WIDE_KEYS = 8192;
 constexpr uint32_t ROWS_LEAST = 8, CHUNK_LEAST = 4;   // tiles of an item: 256 keys
 // Few rows with weights: up to 2^30 scores (rows times room) are kept, a workspace of 4 GiB.  Above
 // that the weights take the chunks' second pass over the keys, which is slower but keeps
@@ -894,20 +899,24 @@ constexpr uint64_t SCORES_MOST = 1ull << 30;
 constexpr uint32_t WEIGHT_ITEMS = 4096;   // with 1024, two rounds of the chip, uneven ends took a quarter of the time
 
 struct AttnPlan {
-    bool few, wide, scores;
+    bool few, wide, ragged, scores;
     uint32_t row_tile, dim, items, slots, slot_rows, weight_parts, key_blocks;
     uint64_t score_stride, score_room;   // scores of a row, and of the call that the workspace holds
 };
-static AttnPlan attn_plan(uint32_t n_seqs, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv, uint32_t dim, bool weights) {
+static AttnPlan attn_plan(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32_t max_kv, uint32_t n_heads, uint32_t n_kv,
+                          uint32_t dim, bool weights) {
     AttnPlan p;
     const uint32_t group = n_heads / n_kv;
     p.few = (uint64_t)max_q * group <= ROWS_MOST;
     p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
-    // an item that is a part has more than half an item's tiles: at most two per item wanted
-    p.wide = !p.few && p.dim == 128 && n_seqs < RAGGED_SEQS && (uint64_t)max_q * group >= WIDE_ROWS && max_kv >= WIDE_KEYS;
+    const uint64_t most = (uint64_t)max_q * group;   // rows of a sequence and head
+    p.wide = !p.few && p.dim == 128 && n_seqs <= WIDE_SEQS && most >= (uint64_t)WIDE_ROWS * n_seqs && max_kv >= WIDE_KEYS;
+    p.ragged = !p.few && n_seqs >= RAGGED_SEQS && (uint64_t)n_rows * 8 < (uint64_t)n_seqs * max_q * 7;
     p.row_tile = p.few ? ROWS_MOST : 32 * (p.wide ? CHUNK_WAVES_WIDE : CHUNK_WAVES);
-    p.items = p.few ? ROWS_ITEMS : p.wide ? CHUNK_ITEMS_WIDE : n_seqs < RAGGED_SEQS ? CHUNK_ITEMS : CHUNK_ITEMS_RAGGED;
-    p.slots = 2 * p.items;
+    p.items = p.few ? ROWS_ITEMS : p.wide ? CHUNK_ITEMS_WIDE : p.ragged ? CHUNK_ITEMS_RAGGED : CHUNK_ITEMS;
+    // an item that is a part has more than half an item's tiles: at most two per item wanted (and
+    // a workspace for many rows holds out for fewer, uneven ones)
+    p.slots = 2 * (!p.few && n_seqs >= RAGGED_SEQS ? CHUNK_ITEMS_RAGGED : p.items);
     p.slot_rows = p.few ? (max_q ? max_q : 1) * group : p.row_tile;
     p.score_stride = ((uint64_t)max_kv + 31) / 32 * 32;
     // a workspace for some bounds holds out for lower ones, so above SCORES_MOST it does not shrink
@@ -1038,7 +1047,7 @@ size_t pc_attn_paged_ws(uint32_t n_seqs, uint32_t n_rows, uint32_t max_q, uint32
     using namespace pc;
     if (!n_heads || !n_kv_heads || n_heads % n_kv_heads) return WS_HEADER;
     AttnArgs a;
-    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, with_weight != 0);
+    const AttnPlan p = attn_plan(n_seqs, n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim, with_weight != 0);
     return attn_carve(&a, p, nullptr, n_seqs, n_rows, max_kv, n_heads, n_kv_heads, with_weight != 0);
 }
 
@@ -1066,7 +1075,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     if (((uint64_t)(uintptr_t)q | (uint64_t)(uintptr_t)out | q_stride_row * 2 | q_stride_head * 2 | out_stride_row * 2 |
          out_stride_head * 2) % 16)
         return PC_ERR_INVALID;
-    const AttnPlan p = attn_plan(n_seqs, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim, weight_out != nullptr);
+    const AttnPlan p = attn_plan(n_seqs, n_rows, max_q, max_kv, n_heads, a.kv.n_kv, a.kv.dim, weight_out != nullptr);
     const size_t need = attn_carve(&a, p, (char *)ws, n_seqs, n_rows, max_kv, n_heads, a.kv.n_kv, weight_out != nullptr);
     const hipStream_t st = (hipStream_t)stream;
     a.table = page_table;
@@ -1095,7 +1104,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.window = window;
     a.by_16 = a.kv.page % 16 == 0 && a.kv.st < (1u << 24);
     a.target = p.items;
-    a.cut_first = p.items == CHUNK_ITEMS_RAGGED;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
+    a.cut_first = p.ragged;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.row_tile;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);

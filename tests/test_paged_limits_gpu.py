@@ -174,3 +174,33 @@ def test_cut_sequences_among_many(n, new, page):
     c = Case(kv, m, heads=8, kvh=2, dim=32, page=page, seed=n + new, weights=True)
     c.check()
     c.check(window=900)
+
+
+@pytest.mark.parametrize("dtype,cache,dim", [(BF16, BF16, 128), (F16, F16, 96), (BF16, FP8, 80)], ids=["bf16", "f16", "fp8"])
+def test_tall_tiles_of_rows(dtype, cache, dim):
+    """Up to three sequences of 2,048 rows (tokens times heads of a group) for each, with room for 8,192 slots."""
+    for kv, new, window in (([1300], [260], 0), ([2200, 530], [520, 300], 0), ([900, 1500, 500], [20, 770, 300], 700)):
+        c = Case(kv, new, heads=8, kvh=1, dim=dim, page=16, dtype=dtype, cache=cache, weights=True, seed=dim + len(kv), cols=512)
+        c.check(window=window)
+
+
+def test_tall_tiles_do_not_show_what_is_masked():
+    c = Case([1400], [300], heads=8, kvh=1, dim=128, page=16, seed=5, cols=512)
+    for j in (1399, 1150, 1200):
+        page, off = int(c.table[0, j // 16]), j % 16
+        c.vc[page, 0, off, 3 + j % 7] = float("nan") if j % 2 else float("inf")
+    page, off = int(c.table[0, 1390 // 16]), 1390 % 16
+    c.kc[page, 0, off, 7] = float("nan")
+    c.check()
+
+
+@pytest.mark.parametrize("n", [12, 16])
+@pytest.mark.parametrize("even", [True, False])
+def test_chunks_of_even_and_uneven_rows(n, even):
+    """From twelve sequences on uneven ones are cut finer, and cut ones come first."""
+    r = np.random.default_rng(n)
+    new = np.full(n, 40) if even else np.concatenate([[40, 0], r.integers(1, 30, n - 2)])
+    kv = new + np.concatenate([r.integers(0, 200, n - 3), [3000, 0, 1500]])
+    c = Case(kv, new, heads=8, kvh=2, dim=64, seed=n, weights=True)
+    c.check()
+    c.check(window=500)

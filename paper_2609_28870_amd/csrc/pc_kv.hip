@@ -37,8 +37,7 @@ pc_status kv_view(const pc_kv_cache *c, KvView *v) {
 // A copy with an index: bound by memory, or for a few tokens by the one launch
 // and its chain of loads (the row's sequence, its length, its page).
 
-constexpr uint32_t APPEND_MANY = 8192;   // rows: as many as the chip holds waves
-constexpr uint32_t APPEND_ROWS = 4;      // of a wave, then
+constexpr uint32_t APPEND_ROWS = 4;   // of a wave, where rows share one
 
 struct AppendArgs {
     KvView kv;
@@ -122,9 +121,9 @@ __device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b, float scale)
     return (uint32_t)w;
 }
 
-// Few rows: a wave each, so that the row's chain of loads is all there is and its
-// addresses are scalar.  MODE 0: the types agree; 1, 2: an 8-bit cache from bf16, f16.
-// 255 rows: 3.6 us; the kernel below takes 8.5 with one row a wave.
+// A wave a row, so that the row's chain of loads is all there is and its addresses are
+// scalar.  MODE 0: the types agree; 1, 2: an 8-bit cache from bf16, f16.
+// bf16, 4 heads of 128: 256 rows 2.8 us, 8,192 rows 7.5 us (33 MB, 4.5 TB/s).
 template <int MODE>
 __global__ __launch_bounds__(256) void append_few_kernel(AppendArgs a) {
     if (blockIdx.x == 0) {
@@ -180,8 +179,8 @@ __device__ __forceinline__ uint32_t wave_seq_of(const uint32_t *__restrict__ q_o
     return lo;
 }
 
-// Many rows: four to a wave, whose lanes take the 16-byte pieces of their cache
-// entries, so that the chain's wait is shared and no lane idles.
+// Four rows to a wave, whose lanes take the 16-byte pieces of their cache entries, so that
+// the chain's wait is shared and no lane idles where a row has few of them.
 // 21,100 rows of bf16 into an 8-bit cache (4 heads of 128, 65 MB): 18 us, 3.6 TB/s (a
 // row a wave: 24.5).
 template <int MODE>
@@ -245,16 +244,28 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     }
 }
 
-static bool append_many(uint32_t n_rows) { return n_rows >= APPEND_MANY; }
-static uint32_t append_groups(uint32_t n_rows) {
-    const uint32_t per = (append_many(n_rows) ? APPEND_ROWS : 1) * (256 / WAVE);
-    return 1 + (n_rows + per - 1) / per;
+// Rows share a wave where their pieces (of 16 bytes in the cache) leave most of one idle.  Us of a wave
+// a row / of four rows a wave, in 24 sequences:
+//   8-bit cache    8 pieces: 64 rows 6.6 / 3.4, 8,192 rows 11.5 / 5.9;  16: 4.0 / 3.4, 10.3 / 6.3;
+//                  32: 64 rows 3.8 / 5.1, 2,048 rows 5.1 / 5.4, 8,192 rows 11.1 / 8.0;  48: 3.8 / 6.7, 7.4 / 8.0
+//                  (4,096), 12.2 / 11.4;  64: 13.6 / 15.2 (8,192), 37.5 / 39.8 (32,768)
+//   16-bit cache   8 pieces: 16,384 rows 9.8 / 17.3, 65,536 rows 35.4 / 32.5 (256 sequences: 32.1 / 23.1);
+//                  32: 10.8 / 19.2, 38.4 / 40.5 (34.8 / 29.7);  64: 13.9 / 23.0, 60.9 / 62.9 (62.9 / 63.5)
+// And 2^26 rows, a wave each, are more than a launch holds.
+static bool append_many(uint32_t n_rows, uint32_t pieces, bool f8) {
+    if (n_rows >= 1u << 26) return true;
+    if (f8) return pieces <= 16 || (pieces < 64 && n_rows >= 8192);
+    return pieces <= 32 && n_rows >= 65536;
+}
+static uint64_t append_groups(uint32_t n_rows, bool many) {
+    const uint32_t per = (many ? APPEND_ROWS : 1) * (256 / WAVE);
+    return 1 + ((uint64_t)n_rows + per - 1) / per;
 }
 
 template <int MODE>
-static pc_status append_run(const AppendArgs &a, hipStream_t st) {
-    const dim3 grid(append_groups(a.n_rows));
-    if (append_many(a.n_rows)) PC_LAUNCH(K_KV_APPEND, append_kernel<MODE>, grid, dim3(256), 0, st, a);
+static pc_status append_run(const AppendArgs &a, bool many, hipStream_t st) {
+    const dim3 grid((unsigned)append_groups(a.n_rows, many));
+    if (many) PC_LAUNCH(K_KV_APPEND, append_kernel<MODE>, grid, dim3(256), 0, st, a);
     else PC_LAUNCH(K_KV_APPEND, append_few_kernel<MODE>, grid, dim3(256), 0, st, a);
     return PC_OK;
 }
@@ -588,7 +599,12 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     if (ok != PC_OK) return ok;
     if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
     if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
-    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u || !launch_fits(append_groups(n_rows), 256))
+    const bool f8 = cache->dtype == PC_FP8_E4M3;
+    a.by_head = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
+    a.pieces = a.by_head.d * a.kv.n_kv;
+    a.by_token = fast_div(a.pieces);
+    const bool many = append_many(n_rows, a.pieces, f8);
+    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u || !launch_fits(append_groups(n_rows, many), 256))
         return PC_ERR_TOO_LARGE;
     if (max_kv > table_stride * a.kv.page) return PC_ERR_INVALID;
     if (!kv_len || !q_off || (max_kv && !page_table) || (n_rows && (!k || !v))) return PC_ERR_INVALID;
@@ -612,11 +628,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     a.v_row = v_stride_row * 2;
     a.v_head = v_stride_head * 2;
     a.status = (int32_t *)ws;
-    a.by_head = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
-    a.pieces = a.by_head.d * a.kv.n_kv;
-    a.by_token = fast_div(a.pieces);
-    if (cache->dtype != PC_FP8_E4M3) return append_run<0>(a, st);
-    return dtype == PC_BF16 ? append_run<1>(a, st) : append_run<2>(a, st);
+    if (!f8) return append_run<0>(a, many, st);
+    return dtype == PC_BF16 ? append_run<1>(a, many, st) : append_run<2>(a, many, st);
 }
 
 size_t pc_kv_evict_ws(uint32_t n_seqs, uint32_t n_kv_heads, uint32_t max_kv) {

@@ -204,3 +204,39 @@ def test_chunks_of_even_and_uneven_rows(n, even):
     c = Case(kv, new, heads=8, kvh=2, dim=64, seed=n, weights=True)
     c.check()
     c.check(window=500)
+
+
+@pytest.mark.parametrize("n_seqs", [1, 300])
+@pytest.mark.parametrize("heads,dim,dtype", [(1, 16, BF16), (4, 64, F16), (5, 64, BF16)])
+def test_append_of_very_many_rows(n_seqs, heads, dim, dtype):
+    """From 65,536 rows on those of small 16-bit entries share waves: every slot, with empty
+    sequences among the others, rows without a slot and a page that is not there."""
+    r = np.random.default_rng(n_seqs + dim)
+    rows, page = 65536 + 5, 10
+    off = np.concatenate([[0], np.sort(r.integers(0, rows + 1, n_seqs - 1)), [rows]])
+    new = np.diff(off)
+    kv = np.maximum(0, new + r.integers(-3, 30, n_seqs))
+    each = (kv + page - 1) // page
+    pages = int(each.sum())
+    table = np.full((n_seqs, int(each.max())), -1, np.int64)
+    order = r.permutation(pages)
+    for s, at in enumerate(np.cumsum(each) - each):
+        table[s, :each[s]] = order[at:at + each[s]]
+    last = int(np.argmax(new))
+    table[last, each[last] // 2] = pages
+    g = torch.Generator(device="cuda").manual_seed(n_seqs)
+    k, v = (torch.zeros((pages, heads, page, dim), dtype=dtype, device="cuda") for _ in range(2))
+    kn, vn = (torch.randn((rows, heads, dim), generator=g, device="cuda").to(dtype) for _ in range(2))
+    seq = np.repeat(np.arange(n_seqs), new)
+    slot = kv[seq] - off[seq + 1] + np.arange(rows)
+    at = table[seq, np.maximum(slot, 0) // page]
+    fine = (slot >= 0) & (at >= 0) & (at < pages)
+    take, to, where = (torch.from_numpy(x[fine]).cuda() for x in (np.arange(rows), at, slot % page))
+    want = [torch.zeros_like(k), torch.zeros_like(v)]
+    for w, x in zip(want, (kn, vn)):
+        w[to, :, where] = x[take]
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")   # noqa: E731
+    ws = pc.kv_append(pc.PagedCache(k, v), i32(table), i32(kv), i32(off), kn, vn)
+    torch.cuda.synchronize()
+    assert pc.workspace_status(ws) == 2
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])

@@ -303,25 +303,38 @@ __device__ __forceinline__ uint32_t slot_of(const AttnArgs &a, const Item &it, u
 
 // ------------------------------------------------------------------ rows
 
+// Elements of a query with the sign of the scores' factor; a factor of zero leaves zeros, and NaN
+// of what is not finite.
+template <class T>
+__device__ __forceinline__ uint32_t times_zero(uint32_t w) {
+    return ((w & T::EXPONENT) == T::EXPONENT ? 0x7FFFu : 0) | ((w >> 16 & T::EXPONENT) == T::EXPONENT ? 0x7FFF0000u : 0);
+}
+template <class T, int N>
+__device__ __forceinline__ void sign_query(uint4 (&q)[N], uint32_t flip, bool zero) {
+    if (zero) {   // rare, and apart, so that the loads before are one run
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            q[i] = make_uint4(times_zero<T>(q[i].x), times_zero<T>(q[i].y), times_zero<T>(q[i].z), times_zero<T>(q[i].w));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = make_uint4(q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip);
+}
 // A row's query as the right operand of scores^T = K Q^T: step s holds dimensions
 // 32 (s / 2) + 16 half + 8 (s % 2) .. + 7, the order in which keys are read, too
 // (the sum over dimensions takes any order that both operands share).
 constexpr __device__ __forceinline__ uint32_t dim_of_step(uint32_t step, uint32_t half) {
     return 32 * (step / 2) + 16 * half + 8 * (step % 2);
 }
-template <int D, bool FULL>
+template <class T, int D, bool FULL>
 __device__ __forceinline__ void load_query(const AttnArgs &a, const char *row, bool there, uint32_t half, uint32_t flip,
                                            bool zero, uint4 (&q)[D / 16]) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
         const uint32_t d = dim_of_step(s, half);
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (there && !zero && (FULL || d < a.kv.dim)) {
-            x = *(const uint4 *)(row + d * 2);
-            x = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-        }
-        q[s] = x;
+        q[s] = make_uint4(0, 0, 0, 0);
+        if (there && (FULL || d < a.kv.dim)) q[s] = *(const uint4 *)(row + d * 2);
     }
+    sign_query<T>(q, flip, zero);
 }
 
 // SLACK in units of scores that are taken times c > 0; finite, so that a first score always

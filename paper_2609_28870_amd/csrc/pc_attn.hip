@@ -176,11 +176,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
     for (int i = 0; i < D / 64; ++i) {
         const uint32_t r = (threadIdx.x + 256 * i) / (D / 8), d = threadIdx.x % (D / 8) * 8, n = a.by_group.div(r);
         q[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows && !zero && (FULL || d < a.kv.dim)) {
-            const uint4 x = *(const uint4 *)(a.q + (uint64_t)(sq.first + n) * a.q_row +
-                                             (it.head * a.group + (r - n * a.group)) * a.q_head + d * 2);
-            q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-        }
+        if (r < rows && (FULL || d < a.kv.dim))
+            q[i] = *(const uint4 *)(a.q + (uint64_t)(sq.first + n) * a.q_row + (it.head * a.group + (r - n * a.group)) * a.q_head + d * 2);
     }
     if (t < t_end) {
         at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
@@ -188,6 +185,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         load(a.kv.v, v);
         if (t + 4 < t_end) look_up(t + 4);
     }
+    sign_query<T>(q, flip, zero);
 #pragma unroll
     for (int i = 0; i < D / 64; ++i)
         *(uint4 *)(queries + piece_at<D>((threadIdx.x + 256 * i) / (D / 8), threadIdx.x % (D / 8))) = q[i];
@@ -363,7 +361,7 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
     const uint64_t past = (uint64_t)from + (uint64_t)it.length * CHUNK_KEYS;
     const uint32_t k_lo = max(from, own.lo & ~(CHUNK_KEYS - 1u)), k_hi = (uint32_t)min((uint64_t)own.hi, past);
     uint4 q[D / 16];
-    load_query<D, FULL>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
+    load_query<T, D, FULL>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
     const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
 
     uint4 k[PIECES], v[PIECES];

@@ -134,3 +134,21 @@ def test_scores_of_minus_infinity_weigh_nothing(new, kv):
     for x, y, t in ((out[:, 2:], want[0][:, 2:], tol[0][:, 2:]), (lse[:, 2:], want[1][:, 2:], tol[1][:, 2:]),
                     (weight[:, 1], want[2][:, 1], tol[2][:, 1])):
         assert np.all(np.abs(x.cpu().double().numpy() - y) <= t)
+
+
+@pytest.mark.parametrize("new", [1, 64])
+@pytest.mark.parametrize("kv", [90, 5000])
+@TYPES
+@pytest.mark.parametrize("broken", [float("nan"), float("inf")])
+def test_a_factor_of_zero_keeps_a_broken_query_broken(new, kv, dtype, cache, broken):
+    """0 * NaN and 0 * infinity are NaN: by a scale of zero, or an 8-bit cache's scale of zero."""
+    c = Case([kv], [new], heads=4, kvh=2, dtype=dtype, cache=cache, seed=kv, weights=True)
+    scale = 0.0
+    if cache == FP8:
+        c.ks[0], scale = 0.0, 0.2
+    want, tol = c.want(scale=scale)
+    rows, slots = np.zeros((new, 4), bool), np.zeros(c.weight.shape, bool)
+    c.q[new // 2, 1, 3] = broken
+    rows[new // 2, 1] = True
+    slots[0, 0, :kv] = visible(c, 0)[new // 2]
+    compare(c.run(scale=scale), want, tol, rows, slots)

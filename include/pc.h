@@ -546,8 +546,8 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  *   lse        float[n_rows * n_heads] or NULL
  *   weight     float, [s][h] rows of max_kv entries, weight_stride apart (s * n_kv_heads + h
  *              times weight_stride), or NULL: zeros; entries from kv_len on count as 0
- *   weight_out the same layout, or NULL: no weights; may be weight.  All max_kv
- *              entries are written, 0 from kv_len on.
+ *   weight_out the same layout, or NULL: no weights; may be weight (else they do not
+ *              overlap).  All max_kv entries are written, 0 from kv_len on.
  *   n_heads    a multiple of n_kv_heads; scale finite
  * With few rows and weights the workspace holds the scores, 4 bytes a new row, query head and
  * slot of max_kv (n_seqs * max_q * n_heads * max_kv in all), or 4 GiB if they are more;

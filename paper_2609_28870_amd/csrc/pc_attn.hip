@@ -1115,6 +1115,8 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     // in place, a row's query is read before its result is written, but for the weights' own pass
     const bool in_place = q == out && same_strides(from, to, n_rows, n_heads) && !weight_out;
     if (!in_place && entries_overlap(from, to, n_rows, n_heads, 2ull * a.kv.dim)) return PC_ERR_INVALID;
+    const uint64_t weight_bytes = max_kv && n_seqs ? (((uint64_t)n_seqs * a.kv.n_kv - 1) * weight_stride + max_kv) * 4 : 0;
+    if (weight && weight != weight_out && overlap(weight, weight_bytes, weight_out, weight_bytes)) return PC_ERR_INVALID;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
     const bool f8 = cache->dtype == PC_FP8_E4M3;
     if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, g, st) : attn_dim<Bf16, false>(a, p, g, st);

@@ -40,3 +40,10 @@ def test_attention_results(L):   # noqa: F811
     heads_first = dict(qr=128, outr=128, qh=640, outh=640)        # [head][row], runs with gaps
     for at in (16, 112, 144, 256, -16):
         refused(FAKE + at, **heads_first)
+
+
+def test_attention_weights(L):   # noqa: F811
+    """3 sequences, 2 heads, 64 weights each: in place or apart."""
+    size, far = 6 * 64 * 4, dict(out=FAKE + 0x10000, wstride=64)
+    for at in (4, 256, size - 4, -4, 4 - size):
+        assert attn(L, w=FAKE + 0x20000, wout=FAKE + 0x20000 + at, **far) == -1

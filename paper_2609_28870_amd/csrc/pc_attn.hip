@@ -116,8 +116,9 @@ __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, co
 // go straight into the matrix product, a lane per key; values pass through
 // LDS for the transposed read.  The four waves' results are joined in LDS.
 // FULL: the head has D dimensions, and no piece of a key is past them.
-// bf16, 32 over 4 heads of 128: 63 sequences, 618k keys 255 us (5.0 TB/s); 8-bit, 1.05M
-// keys 192 us (5.6 TB/s); one token over 1,537 keys 10.5 us, a chain of dependent loads.
+// 32 over 4 heads of 128, 1.05M keys in 8 even sequences: bf16 384 us, 8-bit 194 us (5.6 TB/s; a
+// plain read of 4 GiB: 6.3); 618k keys in 63 uneven ones, bf16, 254 us (5.0 TB/s: ranges end at different
+// times); one token over 1,537 keys 11 us, a chain of dependent loads.
 template <class T, bool F8, int D, bool FULL, bool WEIGHTS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a) {
     constexpr int PIECES = F8 ? D / 32 : D / 16;   // 16 bytes, of one lane's half of a key
@@ -318,8 +319,9 @@ constexpr __host__ __device__ int chunk_keys(int d) { return d <= 128 ? 64 : 32;
 // worked on, and written to the other buffer).  W waves: four and two workgroups to a
 // compute unit, or eight, which load and write half as much a wave for rows that last.
 // Bound by the matrix products and the exponentials between them: 2,048 tokens over
-// 32,768 (bf16, 32 over 4 heads of 128) 1,050 us, 1,014 TFLOP/s (four waves: 1,141); the
-// matrix cores are busy in 43% of the cycles, vector instructions issued in 42%.
+// 32,768 (bf16, 32 over 4 heads of 128) 1,060 to 1,094 us on five devices, 974 to 1,005 TFLOP/s
+// (four waves: a tenth more time); the matrix cores are busy in 43% of the cycles, vector
+// instructions issued in 42%.
 template <class T, bool F8, int D, bool FULL, int W>
 __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
     constexpr int THREADS = W * WAVE, ROWS = 32 * W;
@@ -537,7 +539,8 @@ __device__ __forceinline__ float2 join_stats(const AttnArgs &a, const Item &it, 
 // The parts of some rows of a tile, `teams` of D / 4 lanes to a row, each over every
 // teams-th part; and the whole call's status, for which the workgroups share the
 // table's entries.  Behind those workgroups, with few rows: the weights, from the scores.
-// Bound by its waits (list, statistics, parts): 6 us for one row, 9 for a decode batch.
+// Bound by its waits (list, statistics, parts): 6 us for one row, 9 for a decode batch, 19 with the
+// weights of 32 uneven sequences of up to 16,384 slots (45 MB of scores).
 template <class T, int D>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t joins, uint32_t row_blocks,
                                                    uint32_t key_blocks) {
@@ -687,8 +690,9 @@ constexpr int WEIGHT_KEYS = 256, WEIGHT_ROWS = 64;
 // rows), 64 keys a wave in registers as the right operand of scores = Q K^T, the rows
 // passing through LDS.  With the statistics known there is no running maximum: a
 // register holds one row, so a key's sum is a sum over registers.  Bound by the
-// matrix products and exponentials: 2 x 1,024 tokens over 16,384 (bf16, 32 over 4 heads of
-// 128) 390 us, 680 TFLOP/s; the attention before it, of twice the products, takes 520.
+// matrix products and exponentials (matrix cores busy in 36% of the cycles, vector instructions
+// issued in 57%): 2 x 1,024 tokens over 16,384 (bf16, 32 over 4 heads of 128) 390 us, 680
+// TFLOP/s; the attention before it, of twice the products, takes some 500.
 template <class T, bool F8, int D, bool FULL>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs a, uint32_t key_blocks) {
     constexpr int PIECES = D / 8 * WEIGHT_ROWS / 256;

@@ -205,8 +205,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         for (int u = 0; u < AT_ONCE; ++u) {
             const uint32_t p = p0 + u * WAVE, i = min(a.by_token.div(p), rows - 1), t = t0 + i;
             const uint32_t of = p - i * a.pieces, h = a.by_head.div(of), c = of - h * a.by_head.d;
-            uint32_t s = s0;
-            while (s + 1 < a.n_seqs && a.q_off[s + 1] <= t) ++s;
+            uint32_t s = s0;   // or a later one, behind any number of empty ones
+            if (s + 1 < a.n_seqs && a.q_off[s + 1] <= t) s += 1 + seq_of(a.q_off + s + 1, a.n_seqs - s - 1, t);
             bool bad;
             const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
             const int64_t slot = slot_of_row(a, s, q, t);

@@ -58,10 +58,13 @@ typedef enum {
 #define PC_BF16 0u                 /* element types of a paged cache and its new tokens */
 #define PC_F16 1u
 #define PC_FP8_E4M3 2u             /* 8 bits: 4 of exponent, 3 of fraction, no infinity */
+#define PC_FP4_E2M1 3u             /* 4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; blocks of 32 with a scale */
 #define PC_MAX_PAGE 65536u         /* largest page of a paged cache, in slots */
 #define PC_MAX_HEADS 1024u         /* largest number of query heads */
 #define PC_MAX_HEAD_DIM 256u
 #define PC_ATTN_CAUSAL 1u          /* pc_attn_paged flag */
+#define PC_ROPE_INTERLEAVED 1u     /* pc_rotation flags: neighbours are pairs (else the halves of the turned part) */
+#define PC_ROPE_TRANSPOSE 2u       /* turned the other way: the gradient of what is turned without it */
 
 /* Human-readable name of a status code (static storage). */
 const char *pc_status_string(pc_status s);
@@ -482,10 +485,15 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
  * sequence s is in page page_table[s * table_stride + j / page_size].  A page
  * may stand in the tables of many sequences (a shared prefix).
  *
- *   dtype       PC_BF16, PC_F16, or PC_FP8_E4M3, whose values are the codes
- *               times a scale per head (k_scale, v_scale: float[n_kv_heads];
- *               NULL for the other types)
- *   head_dim    a multiple of 16, at most PC_MAX_HEAD_DIM
+ *   dtype       PC_BF16 or PC_F16 (k_scale and v_scale are NULL);
+ *               PC_FP8_E4M3, whose values are the codes times a scale per head (k_scale,
+ *               v_scale: float[n_kv_heads]);
+ *               PC_FP4_E2M1, two codes a byte (element i in bits 4 (i % 2) .. + 3 of byte
+ *               i / 2), whose values are the codes times 2^(b - 127), b the scale
+ *               byte of their 32 elements (255: NaN): that of elements i .. i + 31, i a
+ *               multiple of 32, is byte i / 32 of k_scale (v_scale), which the calls that
+ *               write k (v) write, too.  Queries of PC_F16 read it rounded to their type.
+ *   head_dim    a multiple of 16 (PC_FP4_E2M1: of 32), at most PC_MAX_HEAD_DIM
  *   k, v and the strides in bytes are multiples of 16
  *
  * Calls on it take new tokens as chunks: rows q_off[s] .. q_off[s+1] - 1 of the
@@ -502,7 +510,7 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
  * ------------------------------------------------------------------------ */
 typedef struct {
     void *k, *v;
-    const float *k_scale, *v_scale;
+    const void *k_scale, *v_scale;
     uint64_t stride_page, stride_head, stride_slot; /* elements */
     uint32_t dtype;
     uint32_t n_pages, page_size, n_kv_heads, head_dim;
@@ -510,10 +518,14 @@ typedef struct {
 
 /* New tokens' keys and values into their slots.
  *   k, v     new rows of `dtype` (PC_BF16 or PC_F16; the cache has the same type or
- *            PC_FP8_E4M3): head h of row t at element t * stride_row + h *
+ *            PC_FP8_E4M3 or PC_FP4_E2M1): head h of row t at element t * stride_row + h *
  *            stride_head, head_dim contiguous; pointers and strides in bytes
  *            multiples of 16.  An 8-bit cache takes x / scale, at most 448 in
  *            magnitude, rounded to the nearest code, ties to even; NaN stays NaN.
+ *            A 4-bit cache takes 32 elements with the smallest power of two as their scale that
+ *            leaves the largest below 7 (between 2^-126 and 2^125; of PC_F16 2^-23 and
+ *            2^13), rounded to the nearest code, ties to even, at most 6 in magnitude: off by half a
+ *            step at most, but above the bounds of the scale.  A NaN makes all 32 NaN.
  * A row without a slot or page is left out (status 2).  Two rows that share a
  * slot (a page in two tables) leave it unspecified. */
 size_t pc_kv_append_ws(void);
@@ -522,6 +534,65 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
                        uint32_t max_kv, const void *k, uint64_t k_stride_row, uint64_t k_stride_head,
                        const void *v, uint64_t v_stride_row, uint64_t v_stride_head, uint32_t dtype, void *ws,
                        size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions: what a token's queries and keys are turned by, so that a cached
+ * key serves every later query of its sequence (Sec. 2.2: the state of a token depends
+ * on the whole sequence before it, its position among it).  Of every head the first
+ * rot_dim dimensions turn, in pairs (a, b): (i, i + rot_dim / 2), or (2 i, 2 i + 1) with
+ * PC_ROPE_INTERLEAVED, i < rot_dim / 2; the others stay as they are.
+ *     y_a = x_a c - x_b s,  y_b = x_b c + x_a s,   (c, s) = table[position][i]
+ * With PC_ROPE_TRANSPOSE s counts as -s: that takes the gradient of y to the gradient
+ * of x, and undoes the rotation where c^2 + s^2 = 1.
+ *
+ *   table    float[n_pos][rot_dim / 2][2], a multiple of 8 bytes
+ *   pos      uint32[n_rows]: the position of every row; NULL: pc_rope, row t is at position t;
+ *            pc_kv_append_rope, at its slot.  Rows whose position is n_pos or more are left out
+ *            (status 2).
+ *   rot_dim  even, 2 .. head_dim
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    const float *table;
+    const uint32_t *pos;
+    uint32_t n_pos, rot_dim, flags;
+} pc_rotation;
+
+/* table[p - first][i] = magnitude * (cos(p freq[i]), sin(p freq[i])), first <= p < first + n_pos.
+ * The angle is a product in 64 bits, the result rounded to 32.
+ *   freq       double[n_freq] in HOST memory, at most 1e6 in magnitude each: what a model stretches for
+ *              contexts longer than it was trained on; read before the call returns
+ *   n_freq     1 .. PC_MAX_HEAD_DIM / 2 (rot_dim / 2)
+ *   magnitude  finite; first + n_pos below 2^32 - 1 */
+pc_status pc_rope_table(const double *freq, uint32_t n_freq, uint64_t first, uint64_t n_pos, double magnitude,
+                        float *table, void *stream);
+
+/* Rows turned by their positions, in 32 bits and rounded to `dtype` (PC_BF16, PC_F16) once.
+ *   x, out    head h of row t at element t * stride_row + h * stride_head, head_dim contiguous
+ *             (a multiple of 8, at most PC_MAX_HEAD_DIM); pointers and strides in bytes
+ *             multiples of 16.  out may be x, with its strides; else they do not overlap.
+ *   n_heads   1 .. PC_MAX_HEADS */
+size_t pc_rope_ws(void);
+pc_status pc_rope(const pc_rotation *rotation, const void *x, uint64_t x_stride_row, uint64_t x_stride_head,
+                  void *out, uint64_t out_stride_row, uint64_t out_stride_head, uint32_t dtype, uint32_t n_rows,
+                  uint32_t n_heads, uint32_t head_dim, void *ws, size_t ws_bytes, void *stream);
+
+/* pc_kv_append of keys that are turned on the way (values are not), and in the same launch the
+ * new tokens' queries.  A cache of the rows' type holds what pc_rope gives; codes of 8 and 4 bits
+ * are taken of the turned value rounded to 32 bits, the sum of its two exact products.
+ *   rotation  not PC_ROPE_TRANSPOSE
+ *   q, q_out  rows like k, n_heads heads of them, and what pc_rope makes of them; both NULL:
+ *             none.  q_out may be q, with its strides; else they do not overlap, and q_out
+ *             shares no memory with k and v (rows of one stride may lie beside each other's).
+ * A row left out for its position, or that has no slot where positions are slots, leaves q_out
+ * untouched, too. */
+size_t pc_kv_append_rope_ws(void);
+pc_status pc_kv_append_rope(const pc_kv_cache *cache, const uint32_t *page_table, uint64_t table_stride,
+                            const uint32_t *kv_len, const uint32_t *q_off, uint32_t n_seqs, uint32_t n_rows,
+                            uint32_t max_kv, const pc_rotation *rotation, const void *k, uint64_t k_stride_row,
+                            uint64_t k_stride_head, const void *v, uint64_t v_stride_row, uint64_t v_stride_head,
+                            const void *q, uint64_t q_stride_row, uint64_t q_stride_head, void *q_out,
+                            uint64_t qo_stride_row, uint64_t qo_stride_head, uint32_t n_heads, uint32_t dtype,
+                            void *ws, size_t ws_bytes, void *stream);
 
 /* Attention of new tokens over the cache (which holds them already).
  *     slots a row in slot x sees: j < kv_len[s], j <= x if PC_ATTN_CAUSAL,
@@ -536,7 +607,7 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  * of the slots that the row sees.  What a row does not see never reaches its outputs,
  * whatever its values.
  *
- *   q, out     `dtype` PC_BF16 or PC_F16 (the cache the same or PC_FP8_E4M3), head e of
+ *   q, out     `dtype` PC_BF16 or PC_F16 (the cache the same, PC_FP8_E4M3 or PC_FP4_E2M1), head e of
  *              row t at element t * stride_row + e * stride_head; pointers and
  *              strides in bytes multiples of 16.  out may be q, with its strides, where no
  *              weights are formed; else they do not overlap

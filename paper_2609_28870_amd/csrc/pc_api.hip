@@ -47,6 +47,9 @@ static const char *kernel_name(KernelId k) {
     case K_BELADY_RANK: return "belady_rank";
     case K_BELADY: return "belady";
     case K_KV_APPEND: return "kv_append";
+    case K_KV_APPEND_TURNED: return "kv_append_rope";
+    case K_ROPE: return "rope";
+    case K_ROPE_TABLE: return "rope_table";
     case K_KV_EVICT_SELECT: return "kv_evict_select";
     case K_KV_EVICT_MOVE: return "kv_evict_move";
     case K_ATTN_ROWS: return "attn_rows";

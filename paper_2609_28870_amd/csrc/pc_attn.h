@@ -32,6 +32,10 @@ struct Bf16 {
     static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w) {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
     }
+    template <int BYTE>
+    static __device__ __forceinline__ uint32_t from_e2m1(uint32_t w, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
+    }
     static constexpr uint32_t SIGNS = 0x80008000u, EXPONENT = 0x7F80u;
     static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
 };
@@ -49,12 +53,33 @@ struct F16 {
     static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w) {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     }
+    template <int BYTE>
+    static __device__ __forceinline__ uint32_t from_e2m1(uint32_t w, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, BYTE));
+    }
     static constexpr uint32_t SIGNS = 0x80008000u, EXPONENT = 0x7C00u;
     static __device__ __forceinline__ float value(uint32_t bits) {
         return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
     }
 };
 
+// How the cache holds its values: in the queries' type, as 8-bit or as 4-bit codes.
+enum class Held { SAME, E4M3, E2M1 };
+// bytes of n elements
+template <Held H>
+constexpr __host__ __device__ __forceinline__ uint32_t held_bytes(uint32_t n) {
+    return H == Held::SAME ? 2 * n : H == Held::E4M3 ? n : n / 2;
+}
+
+// The scale of a block of 4-bit codes is the exponent byte of a number: the conversions take
+// that field alone (0 as 2^-127, 255 as NaN).
+__device__ __forceinline__ float scale_of(uint32_t exponent) { return __uint_as_float(exponent << 23); }
+// eight 4-bit codes as a piece of eight elements
+template <class T>
+__device__ __forceinline__ uint4 expand(uint32_t w, float scale) {
+    return make_uint4(T::template from_e2m1<0>(w, scale), T::template from_e2m1<1>(w, scale), T::template from_e2m1<2>(w, scale),
+                      T::template from_e2m1<3>(w, scale));
+}
 // sixteen 8-bit codes as two pieces of eight elements
 template <class T>
 __device__ __forceinline__ void expand(uint4 x, uint4 *lo, uint4 *hi) {
@@ -119,15 +144,16 @@ struct ValueAt {
         }
     }
 };
-// Where this lane finds its key (or query row) lane % 32 of a tile, step i of its dimensions.
-template <int D>
+// Where this lane finds its key (or query row) lane % 32 of a tile, step i of its dimensions: runs of
+// 16 of them in turn with the other half of the wave, or of 32 (a block of 4-bit codes a lane).
+template <int D, bool BLOCKS = false>
 struct RowAt {
     uint32_t at[D == 64 ? 4 : 8];
     __device__ __forceinline__ RowAt() {
         const uint32_t lane = threadIdx.x & (WAVE - 1);
 #pragma unroll
         for (uint32_t i = 0; i < (D == 64 ? 4 : 8); ++i)
-            at[i] = piece_at<D>(lane % 32, 4 * (i / 2) + 2 * (lane / 32) + i % 2);
+            at[i] = piece_at<D>(lane % 32, BLOCKS ? 8 * (i / 4) + 4 * (lane / 32) + i % 4 : 4 * (i / 2) + 2 * (lane / 32) + i % 2);
     }
     __device__ __forceinline__ uint4 read(const char *tile, int i) const {
         return *(const uint4 *)(tile + at[i % (D == 64 ? 4 : 8)] + i / 8 * 256);

@@ -36,22 +36,27 @@ __device__ __forceinline__ uint4 drop_not_finite(uint4 x, bool *any) {
 // tile is worked on without them, and where there were any they are added here, after
 // the loop, to the rows that see them: key by key, the scores formed again.  Rare,
 // so written for size.  `query` is this lane's row of 16-bit elements.
-template <class T, bool F8, int D, class Query>
+template <class T, Held H, int D, class Query>
 __device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs &a, uint32_t seq, uint32_t head, uint32_t key,
                                                int32_t first, int32_t last, float c, Query query) {
     const uint32_t lane = threadIdx.x & (WAVE - 1), half = lane / 32;
     const uint32_t at = a.kv.by_page.div(key), page = page_of(a.kv, a.table[(uint64_t)seq * a.table_stride + at]);
     const uint64_t entry = entry_at(a.kv, page, key - at * a.kv.page, head);
-    auto element = [&](const char *base, uint32_t d) {
-        if (F8) return T::value(T::template from_e4m3<false>(*(const uint8_t *)(base + entry + d)) & 0xFFFF);
-        return T::value(*(const uint16_t *)(base + entry + 2 * d));
+    auto element = [&](bool value, uint32_t d) {
+        const char *x = (value ? a.kv.v : a.kv.k) + entry + held_bytes<H>(d);
+        if (H == Held::E4M3) return T::value(T::template from_e4m3<false>(*(const uint8_t *)x) & 0xFFFF);
+        if (H == Held::E2M1) {
+            const float scale = scale_of((value ? a.kv.v_exp : a.kv.k_exp)[entry / 16 + d / 32]);
+            return T::value(T::template from_e2m1<0>(*(const uint8_t *)x >> 4 * (d % 2), scale) & 0xFFFF);
+        }
+        return T::value(*(const uint16_t *)x);
     };
     bool odd = false;
-    for (uint32_t d = lane; d < a.kv.dim; d += WAVE) odd |= !(fabsf(element(a.kv.v, d)) < __builtin_inff());
+    for (uint32_t d = lane; d < a.kv.dim; d += WAVE) odd |= !(fabsf(element(true, d)) < __builtin_inff());
     if (!ballot(odd)) return;
     float s = 0.f;
 #pragma unroll 1
-    for (uint32_t d = half; d < a.kv.dim; d += 2) s = fmaf(T::value(query(d)), element(a.kv.k, d), s);
+    for (uint32_t d = half; d < a.kv.dim; d += 2) s = fmaf(T::value(query(d)), element(false, d), s);
     s = sum_of_halves(s);
     const float p = exp2_fast(fmaf(s, c, T::TOP - state.m * c));
     const bool visible = (int32_t)key >= first && (int32_t)key <= last;
@@ -60,7 +65,7 @@ __device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const uint32_t d = 32 * b + key_of(r, half);
-            const float x = element(a.kv.v, d < a.kv.dim ? d : 0);
+            const float x = element(true, d < a.kv.dim ? d : 0);
             state.o[b][r] += visible && !(fabsf(x) < __builtin_inff()) ? p * x : 0.f;
             if (r % 4 == 3) __asm__ volatile("" ::: "memory");   // few of the loads at once: the registers are full
         }
@@ -119,9 +124,12 @@ __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, co
 // 32 over 4 heads of 128, 1.05M keys in 8 even sequences: bf16 384 us, 8-bit 194 us (5.6 TB/s; a
 // plain read of 4 GiB: 6.3); 618k keys in 63 uneven ones, bf16, 254 us (5.0 TB/s: ranges end at different
 // times); one token over 1,537 keys 11 us, a chain of dependent loads.
-template <class T, bool F8, int D, bool FULL, bool WEIGHTS>
+template <class T, Held H, int D, bool FULL, bool WEIGHTS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a) {
-    constexpr int PIECES = F8 ? D / 32 : D / 16;   // 16 bytes, of one lane's half of a key
+    constexpr bool F8 = H == Held::E4M3, F4 = H == Held::E2M1;
+    constexpr int PIECES = held_bytes<H>(D) / 32;   // 16 bytes, of one lane's half of a key
+    constexpr int STEPS = D / 16 / PIECES;          // of the product, that a piece serves
+    constexpr int WORDS = (D + 127) / 128;          // of a key's scales (4-bit)
     __shared__ __attribute__((aligned(16))) char tiles[4 * 32 * D * 2];
     __shared__ __attribute__((aligned(16))) char queries[32 * D * 2];   // the same for all waves
     __shared__ float2 join_ml[2][64];
@@ -162,15 +170,35 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         entry = table[p];
     };
     auto load = [&](const char *base, uint4 (&x)[PIECES]) {
-        const char *p = base + at + half * (F8 ? 16 : 32);
+        const char *p = base + at + half * (H == Held::SAME ? 32 : 16);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t o = F8 ? 32 * i : 2 * dim_of_step(i, 0);
+            const uint32_t o = H == Held::SAME ? 2 * dim_of_step(i, 0) : 32 * i;
             // past the head's dimensions: its first ones
-            if (FULL || o + half * (F8 ? 16 : 32) < a.kv.dim * (F8 ? 1 : 2)) x[i] = *(const uint4 *)(p + o);
+            if (FULL || o + half * (H == Held::SAME ? 32 : 16) < held_bytes<H>(a.kv.dim)) x[i] = *(const uint4 *)(p + o);
             else x[i] = *(const uint4 *)(base + at);
         }
     };
+    // Scales of the key at hand: this lane's blocks (every other one) are bytes 0 and 2 of a word.
+    uint32_t ke[WORDS], ve[WORDS];
+    auto load_scales = [&](const uint8_t *base, uint32_t (&e)[WORDS]) {
+        if (!F4) return;
+        const uint8_t *p = base + at / 16;
+        if (FULL) {
+            uint32_t x[WORDS] = {};
+            __builtin_memcpy(x, p, D / 32);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) e[i] = x[i] >> 8 * half;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) e[i] = 0;
+#pragma unroll
+            for (int i = 0; i < (F4 ? PIECES : 0); ++i)
+                if (2 * i + half < a.kv.dim / 32) e[i / 2] |= (uint32_t)p[2 * i + half] << 16 * (i % 2);
+        }
+    };
+    auto scale = [&](const uint32_t (&e)[WORDS], int i) { return scale_of(e[i / 2 % WORDS] >> 16 * (i % 2) & 0xFF); };
+    auto word = [](uint4 x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
     if (t < t_end) look_up(t);
     uint4 q[D / 64];
 #pragma unroll
@@ -183,7 +211,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
     if (t < t_end) {
         at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
         load(a.kv.k, k);
+        load_scales(a.kv.k_exp, ke);
         load(a.kv.v, v);
+        load_scales(a.kv.v_exp, ve);
         if (t + 4 < t_end) look_up(t + 4);
     }
     sign_query<T>(q, flip, zero);
@@ -192,7 +222,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         *(uint4 *)(queries + piece_at<D>((threadIdx.x + 256 * i) / (D / 8), threadIdx.x % (D / 8))) = q[i];
     __syncthreads();
     bool odd = false;   // a value that is not finite was left out of a tile
-    const RowAt<D> q_at;
+    const RowAt<D, F4> q_at;
     const ValueAt<D> v_at;
     const float slack = slack_of<T>(c);
     auto query = [&](int i) { return q_at.read(queries, i); };
@@ -204,30 +234,37 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         if (!FULL) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                if ((F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
+                if ((F4 ? 64 * i + 32 * half : F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            if (F8) {
+            const uint4 &piece = k[i / STEPS];
+            if (F4) {
+                s[0] = T::mfma(expand<T>(word(piece, i % 4), scale(ke, i / STEPS)), query(i), i ? s[0] : f32x16(0.f));
+            } else if (F8) {
                 uint4 x, y;
-                expand<T>(k[i / 2], &x, &y);
+                expand<T>(piece, &x, &y);
                 s[0] = T::mfma(i % 2 ? y : x, query(i), i ? s[0] : f32x16(0.f));
             } else {
-                s[0] = T::mfma(k[i % PIECES], query(i), i ? s[0] : f32x16(0.f));
+                s[0] = T::mfma(piece, query(i), i ? s[0] : f32x16(0.f));
             }
         }
         if (more) {
             at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
             load(a.kv.k, k);
+            load_scales(a.kv.k_exp, ke);
         }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t n = F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
+            const uint32_t n = F4 ? 8 * i + 4 * half : F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
             auto put = [&](uint4 x, int e) {
                 if (!full) x = drop_not_finite<T>(x, &odd);
                 *(uint4 *)(tile + piece_at<D>(col, n + e)) = x;
             };
-            if (F8) {
+            if (F4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) put(expand<T>(word(v[i], e), scale(ve, i)), e);
+            } else if (F8) {
                 uint4 x, y;
                 expand<T>(v[i], &x, &y);
                 put(x, 0);
@@ -238,6 +275,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         }
         if (more) {
             load(a.kv.v, v);
+            load_scales(a.kv.v_exp, ve);
             if (t + 8 < t_end) look_up(t + 8);
         }
         if (!full) {
@@ -266,7 +304,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
             const uint32_t k0 = it.shape.keys.lo + t * 32;
             if ((int32_t)k0 >= all_first && (int32_t)k0 + 31 <= all_last) continue;
             for (uint32_t key = k0; key < min(k0 + 32, it.shape.keys.hi); ++key)
-                add_not_finite<T, F8, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
+                add_not_finite<T, H, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
                     return *(const uint16_t *)(queries + piece_at<D>(col, d / 8) + d % 8 * 2);
                 });
         }
@@ -322,11 +360,12 @@ constexpr __host__ __device__ int chunk_keys(int d) { return d <= 128 ? 64 : 32;
 // 32,768 (bf16, 32 over 4 heads of 128) 1,060 to 1,094 us on five devices, 974 to 1,005 TFLOP/s
 // (four waves: a tenth more time); the matrix cores are busy in 43% of the cycles, vector
 // instructions issued in 42%.
-template <class T, bool F8, int D, bool FULL, int W>
+template <class T, Held H, int D, bool FULL, int W>
 __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnArgs a) {
     constexpr int THREADS = W * WAVE, ROWS = 32 * W;
     constexpr int CHUNK_KEYS = chunk_keys(D), BLOCKS = CHUNK_KEYS / 32;
-    constexpr int PER_ROW = F8 ? D / 16 : D / 8;            // 16-byte pieces of a cache entry
+    constexpr bool CODES = H != Held::SAME;
+    constexpr int PER_ROW = CODES ? D / 16 : D / 8;         // pieces of a cache entry: 16 bytes (of 4-bit codes 8)
     constexpr int PIECES = CHUNK_KEYS * PER_ROW / THREADS;      // of one thread
     constexpr int TILE = CHUNK_KEYS * D * 2;
     static_assert(PIECES * THREADS == CHUNK_KEYS * PER_ROW, "whole pieces");
@@ -366,13 +405,15 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
     load_query<T, D, FULL>(a, a.q + (uint64_t)(sq.first + token) * a.q_row + head * a.q_head, valid, half, flip, zero, q);
     const uint32_t *table = a.table + (uint64_t)it.seq * a.table_stride;
 
-    uint4 k[PIECES], v[PIECES];
+    typedef std::conditional_t<H == Held::E2M1, uint2, uint4> Piece;
+    Piece k[PIECES], v[PIECES];
+    uint32_t ke[PIECES], ve[PIECES];   // exponent bytes of 4-bit codes' scales
     // Where a page holds whole groups of 16 slots, a wave's rows of a piece lie in one group and
     // its address is one number for the wave: the table's entries are read 64 groups at a time,
     // a lane each, and the arithmetic is scalar.  Else every thread finds its rows' pages.
     const uint32_t n_piece = tid % PER_ROW;
-    const bool past_dim = !FULL && n_piece * 16 >= a.kv.dim * (F8 ? 1 : 2);
-    const uint32_t o_piece = past_dim ? 0 : n_piece * 16, o_lane = lane / PER_ROW * (uint32_t)a.kv.st + o_piece;
+    const bool past_dim = !FULL && n_piece * sizeof(Piece) >= held_bytes<H>(a.kv.dim);
+    const uint32_t o_piece = past_dim ? 0 : n_piece * (uint32_t)sizeof(Piece), o_lane = lane / PER_ROW * (uint32_t)a.kv.st + o_piece;
     const uint32_t g_last = (k_hi - 1) / 16;
     uint32_t groups = 0, groups_next = 0, g0 = k_lo / 16;   // entries of groups g0 + lane, g0 + 64 + lane
     uint32_t entry[PIECES], off[PIECES];
@@ -399,16 +440,24 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
                 const uint32_t p = a.kv.by_page.div(slot);
                 const uint32_t page = page_of(a.kv, from_lane(groups, (int)(g - g0)));
                 const uint64_t at = entry_at(a.kv, page, slot - p * a.kv.page + r % 16, it.head);
-                k[i] = *(const uint4 *)(a.kv.k + at + o_lane);
-                v[i] = *(const uint4 *)(a.kv.v + at + o_lane);
+                k[i] = *(const Piece *)(a.kv.k + at + o_lane);
+                v[i] = *(const Piece *)(a.kv.v + at + o_lane);
+                if (H == Held::E2M1) {
+                    ke[i] = a.kv.k_exp[at / 16 + o_lane / 16];
+                    ve[i] = a.kv.v_exp[at / 16 + o_lane / 16];
+                }
             }
             return;
         }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint64_t at = entry_at(a.kv, page_of(a.kv, entry[i]), off[i], it.head) + o_piece;
-            k[i] = *(const uint4 *)(a.kv.k + at);
-            v[i] = *(const uint4 *)(a.kv.v + at);
+            k[i] = *(const Piece *)(a.kv.k + at);
+            v[i] = *(const Piece *)(a.kv.v + at);
+            if (H == Held::E2M1) {
+                ke[i] = a.kv.k_exp[at / 16];
+                ve[i] = a.kv.v_exp[at / 16];
+            }
         }
     };
     auto is_edge = [&](uint32_t k0) {
@@ -416,9 +465,9 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
     };
     if (tid == 0) odd = 0;
     __syncthreads();
-    uint32_t to[F8 ? 2 : 1];   // this thread's places in a tile
+    uint32_t to[CODES ? 2 : 1];   // this thread's places in a tile
 #pragma unroll
-    for (int e = 0; e < (F8 ? 2 : 1); ++e) to[e] = piece_at<D>(tid / PER_ROW, n_piece * (F8 ? 2 : 1) + e);
+    for (int e = 0; e < (CODES ? 2 : 1); ++e) to[e] = piece_at<D>(tid / PER_ROW, n_piece * (CODES ? 2 : 1) + e);
     auto store = [&](int buf, uint32_t k0) {
         const bool edge = is_edge(k0);
         bool mine = false;
@@ -436,12 +485,16 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
                 *(uint4 *)(lds[buf][0] + o) = x;
                 *(uint4 *)(lds[buf][1] + o) = y;
             };
-            if (F8) {
+            if constexpr (H == Held::E2M1) {
+                const float x = scale_of(ke[i]), y = scale_of(ve[i]);
+                put(expand<T>(k[i].x, x), expand<T>(v[i].x, y), 0);
+                put(expand<T>(k[i].y, x), expand<T>(v[i].y, y), 1);
+            } else if constexpr (H == Held::E4M3) {
                 uint4 x0, x1, y0, y1;
                 expand<T>(k[i], &x0, &x1);
                 expand<T>(v[i], &y0, &y1);
                 put(x0, y0, 0);
-                put(x1, y1, F8 ? 1 : 0);
+                put(x1, y1, 1);
             } else {
                 put(k[i], v[i], 0);
             }
@@ -500,7 +553,7 @@ __global__ __launch_bounds__(W * WAVE, D <= 128 ? 2 : 1) void chunk_kernel(AttnA
         for (uint32_t k0 = k_lo; k0 < k_hi; k0 += CHUNK_KEYS) {
             if (!is_edge(k0)) continue;
             for (uint32_t key = k0; key < min(k0 + CHUNK_KEYS, k_hi); ++key)
-                add_not_finite<T, F8, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
+                add_not_finite<T, H, D>(state, a, it.seq, it.head, key, first, last, c, [&](uint32_t d) {
                     return zero ? 0u : *(const uint16_t *)(row_q + 2 * d) ^ (flip & 0x8000u);
                 });
         }
@@ -693,7 +746,7 @@ constexpr int WEIGHT_KEYS = 256, WEIGHT_ROWS = 64;
 // matrix products and exponentials (matrix cores busy in 36% of the cycles, vector instructions
 // issued in 57%): 2 x 1,024 tokens over 16,384 (bf16, 32 over 4 heads of 128) 390 us, 680
 // TFLOP/s; the attention before it, of twice the products, takes some 500.
-template <class T, bool F8, int D, bool FULL>
+template <class T, Held H, int D, bool FULL>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs a, uint32_t key_blocks) {
     constexpr int PIECES = D / 8 * WEIGHT_ROWS / 256;
     constexpr int TILE = WEIGHT_ROWS * D * 2;
@@ -732,15 +785,25 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void weight_kernel(AttnArgs 
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 const uint32_t j = min(k0 + wave * 64 + 32 * n + col, k_hi - 1), p = a.kv.by_page.div(j);
-                const char *base = a.kv.k + entry_at(a.kv, page_of(a.kv, table[p]), j - p * a.kv.page, h);
+                const uint64_t entry = entry_at(a.kv, page_of(a.kv, table[p]), j - p * a.kv.page, h);
+                const char *base = a.kv.k + entry;
 #pragma unroll
-                for (int i = 0; i < D / 16; i += F8 ? 2 : 1) {
-                    const uint32_t d = dim_of_step(i, half), size = F8 ? 1 : 2;
+                for (int i = 0; i < D / 16; i += H == Held::SAME ? 1 : 2) {
+                    const uint32_t d = dim_of_step(i, half);
                     const bool in = FULL || d < a.kv.dim;
-                    uint4 x = *(const uint4 *)(base + (in ? d * size : 0));
-                    if (!in) x = make_uint4(0, 0, 0, 0);
-                    if (F8) expand<T>(x, &k[n][i], &k[n][i + (F8 ? 1 : 0)]);
-                    else k[n][i] = x;
+                    const char *from = base + (in ? held_bytes<H>(d) : 0);
+                    const uint32_t all = in ? ~0u : 0;
+                    if constexpr (H == Held::E2M1) {
+                        const uint2 x = *(const uint2 *)from;
+                        const float s = scale_of(a.kv.k_exp[entry / 16 + (in ? d / 32 : 0)]);
+                        k[n][i] = expand<T>(x.x & all, in ? s : 1.f);
+                        k[n][i + 1] = expand<T>(x.y & all, in ? s : 1.f);
+                    } else {
+                        uint4 x = *(const uint4 *)from;
+                        x = make_uint4(x.x & all, x.y & all, x.z & all, x.w & all);
+                        if constexpr (H == Held::E4M3) expand<T>(x, &k[n][i], &k[n][i + 1]);
+                        else k[n][i] = x;
+                    }
                 }
             }
             // the scale's sign, or its zero, goes to the keys; and they are waited for here, else
@@ -983,61 +1046,38 @@ static bool attn_fits(const AttnGrids &g, const AttnPlan &p) {
     return launch_fits(g.items, p.few ? 256 : p.row_tile / 32 * WAVE) && launch_fits(g.joins + g.weigh, 256) && launch_fits(g.weights, 256);
 }
 
-template <class T, bool F8, int D, bool FULL>
+template <class T, Held H, int D, bool FULL>
 static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
     const dim3 items((unsigned)g.items);
     if (p.few) {
-        if (p.scores) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, true>), items, dim3(256), 0, st, a);
-        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, F8, D, FULL, false>), items, dim3(256), 0, st, a);
+        if (p.scores) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, true>), items, dim3(256), 0, st, a);
+        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, false>), items, dim3(256), 0, st, a);
     } else if (p.wide) {
         constexpr int W = D == 128 ? CHUNK_WAVES_WIDE : CHUNK_WAVES;
-        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL, W>), items, dim3(W * WAVE), 0, st, a);
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, H, D, FULL, W>), items, dim3(W * WAVE), 0, st, a);
     } else {
-        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, F8, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
+        PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, H, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
     }
     PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(g.joins + g.weigh)), dim3(256), 0, st, a, g.teams, (uint32_t)g.joins,
               g.row_blocks, g.key_blocks);
     if (g.weights) {
-        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, F8, D, FULL>), dim3((unsigned)g.weights), dim3(256), 0, st, a, p.key_blocks);
+        PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, H, D, FULL>), dim3((unsigned)g.weights), dim3(256), 0, st, a, p.key_blocks);
         if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)g.sums), dim3(256), 0, st, a, p.key_blocks);
     }
     return PC_OK;
 }
-template <class T, bool F8>
+template <class T, Held H>
 static pc_status attn_dim(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
     const bool full = a.kv.dim == p.dim;
-    if (p.dim == 64) return full ? attn_run<T, F8, 64, true>(a, p, g, st) : attn_run<T, F8, 64, false>(a, p, g, st);
-    if (p.dim == 128) return full ? attn_run<T, F8, 128, true>(a, p, g, st) : attn_run<T, F8, 128, false>(a, p, g, st);
-    return full ? attn_run<T, F8, 256, true>(a, p, g, st) : attn_run<T, F8, 256, false>(a, p, g, st);
+    if (p.dim == 64) return full ? attn_run<T, H, 64, true>(a, p, g, st) : attn_run<T, H, 64, false>(a, p, g, st);
+    if (p.dim == 128) return full ? attn_run<T, H, 128, true>(a, p, g, st) : attn_run<T, H, 128, false>(a, p, g, st);
+    return full ? attn_run<T, H, 256, true>(a, p, g, st) : attn_run<T, H, 256, false>(a, p, g, st);
 }
 
-// Two arrays [n_rows][n_heads] of runs of `width` bytes: whether they are one, and whether they
-// share memory.  In one range they are known not to if their strides agree and one lies in the
-// other's gaps, between its runs or between blocks of them.
-struct Entries {
-    const void *base;
-    uint64_t row, head;   // strides in bytes
-};
-static bool same_strides(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads) {
-    return (n_rows < 2 || x.row == y.row) && (n_heads < 2 || x.head == y.head);
-}
-static bool entries_overlap(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads, uint64_t width) {
-    if (!n_rows) return false;
-    auto extent = [&](const Entries &e) { return (n_rows - 1) * e.row + (n_heads - 1) * e.head + width; };
-    if (!overlap(x.base, extent(x), y.base, extent(y))) return false;
-    if (!same_strides(x, y, n_rows, n_heads)) return true;
-    const uint64_t apart = (uint64_t)(uintptr_t)y.base - (uint64_t)(uintptr_t)x.base, back = 0 - apart;
-    auto in_gaps = [&](uint64_t stride, uint64_t size) {   // of blocks of `size` bytes a stride apart
-        if (!stride) return false;
-        const uint64_t d = (int64_t)apart < 0 ? (stride - back % stride) % stride : apart % stride;
-        return d >= size && d + size <= stride;
-    };
-    if (n_rows < 2 && n_heads < 2) return true;
-    if (n_rows < 2 || n_heads < 2) return !in_gaps(n_rows < 2 ? x.head : x.row, width);
-    const bool by_row = x.head <= x.row;   // the heads of a row make a block, or the rows of a head
-    const uint64_t inner = by_row ? x.head : x.row, outer = by_row ? x.row : x.head, n = by_row ? n_heads : n_rows;
-    if (inner && outer % inner == 0 && in_gaps(inner, width)) return false;
-    return !in_gaps(outer, (n - 1) * inner + width);
+template <class T>
+static pc_status attn_held(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, Held held, hipStream_t st) {
+    if (held == Held::E2M1) return attn_dim<T, Held::E2M1>(a, p, g, st);
+    return held == Held::E4M3 ? attn_dim<T, Held::E4M3>(a, p, g, st) : attn_dim<T, Held::SAME>(a, p, g, st);
 }
 
 }  // namespace pc
@@ -1065,7 +1105,7 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     const pc_status ok = kv_view(cache, &a.kv);
     if (ok != PC_OK) return ok;
     if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
-    if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
+    if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3 && cache->dtype != PC_FP4_E2M1) return PC_ERR_INVALID;
     if (!n_heads || n_heads > PC_MAX_HEADS || n_heads % a.kv.n_kv || flags & ~PC_ATTN_CAUSAL || !isfinite(scale))
         return PC_ERR_INVALID;
     if (max_kv > 0x7FFF0000u || (uint64_t)n_rows * n_heads > 0x7FFFFFFFu || (uint64_t)max_q * n_heads > 0x7FFFFFFFu)
@@ -1122,9 +1162,8 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     const uint64_t weight_bytes = max_kv && n_seqs ? (((uint64_t)n_seqs * a.kv.n_kv - 1) * weight_stride + max_kv) * 4 : 0;
     if (weight && weight != weight_out && overlap(weight, weight_bytes, weight_out, weight_bytes)) return PC_ERR_INVALID;
     if (n_seqs == 0) return fill_u32((uint32_t *)ws, 0, 1, st);
-    const bool f8 = cache->dtype == PC_FP8_E4M3;
-    if (dtype == PC_BF16) return f8 ? attn_dim<Bf16, true>(a, p, g, st) : attn_dim<Bf16, false>(a, p, g, st);
-    return f8 ? attn_dim<F16, true>(a, p, g, st) : attn_dim<F16, false>(a, p, g, st);
+    const Held held = cache->dtype == PC_FP8_E4M3 ? Held::E4M3 : cache->dtype == PC_FP4_E2M1 ? Held::E2M1 : Held::SAME;
+    return dtype == PC_BF16 ? attn_held<Bf16>(a, p, g, held, st) : attn_held<F16>(a, p, g, held, st);
 }
 
 }  // extern "C"

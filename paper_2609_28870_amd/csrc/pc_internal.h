@@ -77,6 +77,9 @@ enum KernelId {
     K_BELADY_RANK,
     K_BELADY,
     K_KV_APPEND,
+    K_KV_APPEND_TURNED,
+    K_ROPE,
+    K_ROPE_TABLE,
     K_KV_EVICT_SELECT,
     K_KV_EVICT_MOVE,
     K_ATTN_ROWS,

@@ -5,31 +5,65 @@
 
 namespace pc {
 
-size_t type_size(uint32_t dtype) {
+uint64_t bytes_of(uint32_t dtype, uint64_t elements) {
     switch (dtype) {
     case PC_BF16:
-    case PC_F16: return 2;
-    case PC_FP8_E4M3: return 1;
+    case PC_F16: return 2 * elements;
+    case PC_FP8_E4M3: return elements;
+    case PC_FP4_E2M1: return elements / 2;
     }
     return 0;
 }
 
+bool same_strides(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads) {
+    return (n_rows < 2 || x.row == y.row) && (n_heads < 2 || x.head == y.head);
+}
+bool entries_overlap(const Entries &x, const Entries &y, uint64_t n_rows, uint64_t n_heads, uint64_t width) {
+    if (!n_rows) return false;
+    auto extent = [&](const Entries &e) { return (n_rows - 1) * e.row + (n_heads - 1) * e.head + width; };
+    if (!overlap(x.base, extent(x), y.base, extent(y))) return false;
+    if (!same_strides(x, y, n_rows, n_heads)) return true;
+    const uint64_t apart = (uint64_t)(uintptr_t)y.base - (uint64_t)(uintptr_t)x.base, back = 0 - apart;
+    auto in_gaps = [&](uint64_t stride, uint64_t size) {   // of blocks of `size` bytes a stride apart
+        if (!stride) return false;
+        const uint64_t d = (int64_t)apart < 0 ? (stride - back % stride) % stride : apart % stride;
+        return d >= size && d + size <= stride;
+    };
+    if (n_rows < 2 && n_heads < 2) return true;
+    if (n_rows < 2 || n_heads < 2) return !in_gaps(n_rows < 2 ? x.head : x.row, width);
+    const bool by_row = x.head <= x.row;   // the heads of a row make a block, or the rows of a head
+    const uint64_t inner = by_row ? x.head : x.row, outer = by_row ? x.row : x.head, n = by_row ? n_heads : n_rows;
+    if (inner && outer % inner == 0 && in_gaps(inner, width)) return false;
+    return !in_gaps(outer, (n - 1) * inner + width);
+}
+
 pc_status kv_view(const pc_kv_cache *c, KvView *v) {
     if (!c || !c->k || !c->v) return PC_ERR_INVALID;
-    const size_t size = type_size(c->dtype);
-    if (!size) return PC_ERR_INVALID;
-    const bool scaled = c->dtype == PC_FP8_E4M3;
-    if (scaled != (c->k_scale != nullptr) || scaled != (c->v_scale != nullptr)) return PC_ERR_INVALID;
+    const uint64_t run = bytes_of(c->dtype, 32);   // of 32 elements
+    if (!run) return PC_ERR_INVALID;
+    const bool f8 = c->dtype == PC_FP8_E4M3, f4 = c->dtype == PC_FP4_E2M1;
+    if ((f8 || f4) != (c->k_scale != nullptr) || (f8 || f4) != (c->v_scale != nullptr)) return PC_ERR_INVALID;
     if (c->page_size < 1 || c->page_size > PC_MAX_PAGE || c->n_kv_heads < 1 || c->n_kv_heads > PC_MAX_HEADS)
         return PC_ERR_INVALID;
-    if (c->head_dim < 16 || c->head_dim > PC_MAX_HEAD_DIM || c->head_dim % 16 || c->n_pages < 1) return PC_ERR_INVALID;
+    if (c->head_dim < 16 || c->head_dim > PC_MAX_HEAD_DIM || c->head_dim % (f4 ? 32 : 16) || c->n_pages < 1) return PC_ERR_INVALID;
     if (c->n_pages == PC_NONE) return PC_ERR_TOO_LARGE;
-    // every access is of 16 bytes at a multiple of 16
-    const uint64_t bits = (uint64_t)(uintptr_t)c->k | (uint64_t)(uintptr_t)c->v | c->stride_page * size |
-                          c->stride_head * size | c->stride_slot * size;
-    if (bits % 16) return PC_ERR_INVALID;
-    *v = KvView{(char *)c->k, (char *)c->v, c->k_scale, c->v_scale, c->stride_page * size, c->stride_head * size,
-                c->stride_slot * size, c->n_pages, c->n_kv_heads, c->head_dim, c->page_size, fast_div(c->page_size)};
+    // every access is of 16 bytes at a multiple of 16 (and of 4-bit codes a block's)
+    const uint64_t strides = c->stride_page | c->stride_head | c->stride_slot;
+    if (((uint64_t)(uintptr_t)c->k | (uint64_t)(uintptr_t)c->v) % 16 || strides % (512 / run)) return PC_ERR_INVALID;
+    *v = KvView{(char *)c->k,
+                (char *)c->v,
+                f8 ? (const float *)c->k_scale : nullptr,
+                f8 ? (const float *)c->v_scale : nullptr,
+                f4 ? (uint8_t *)const_cast<void *>(c->k_scale) : nullptr,
+                f4 ? (uint8_t *)const_cast<void *>(c->v_scale) : nullptr,
+                bytes_of(c->dtype, c->stride_page),
+                bytes_of(c->dtype, c->stride_head),
+                bytes_of(c->dtype, c->stride_slot),
+                c->n_pages,
+                c->n_kv_heads,
+                c->head_dim,
+                c->page_size,
+                fast_div(c->page_size)};
     return PC_OK;
 }
 
@@ -39,11 +73,7 @@ pc_status kv_view(const pc_kv_cache *c, KvView *v) {
 
 constexpr uint32_t APPEND_ROWS = 4;   // of a wave, where rows share one
 
-struct AppendArgs {
-    KvView kv;
-    const uint32_t *table, *kv_len, *q_off;
-    uint64_t table_stride;
-    uint32_t n_seqs, n_rows, max_kv;
+struct AppendArgs : Chunks {
     const char *k, *v;   // strides in bytes
     uint64_t k_row, k_head, v_row, v_head;
     int32_t *status;
@@ -52,73 +82,15 @@ struct AppendArgs {
     uint32_t pieces;     // of one token
 };
 
-// One word for the whole call, by the first workgroup: it looks at every
-// sequence and every page that the call writes (a lane per page, 64 sequences at
-// a time), so that no launch is spent on clearing a word that the others would set.
 __device__ void append_status(const AppendArgs &a) {
-    __shared__ int32_t wrong;
-    if (threadIdx.x == 0) wrong = 0;
-    __syncthreads();
-    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE, waves = blockDim.x / WAVE;
-    bool any = threadIdx.x == 0 && (a.q_off[0] != 0 || a.q_off[a.n_seqs] != a.n_rows);
-    for (uint32_t s0 = wave * WAVE; s0 < a.n_seqs; s0 += waves * WAVE) {
-        const uint32_t s = s0 + lane;
-        uint32_t from = 0, pages = 0;
-        bool bad = false;
-        if (s < a.n_seqs) {
-            const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
-            bad |= q.rows > q.len;
-            if (q.rows && q.len) {
-                from = a.kv.by_page.div(q.rows < q.len ? q.len - q.rows : 0);
-                pages = a.kv.by_page.div(q.len - 1) + 1 - from;
-            }
-        }
-        any |= bad;
-        // Pages are counted in 32 bits, which rows that overlap (offsets that decrease) could pass, and
-        // the loop below would not end; but then the status is known.
-        if (ballot(bad)) continue;
-        const uint32_t end = wave_incl_scan(pages), all = (uint32_t)__shfl((int)end, WAVE - 1, WAVE);
-        for (uint32_t p0 = 0; p0 < all; p0 += WAVE) {
-            const uint32_t p = p0 + lane;
-            int at = 0;   // sequence of page p: the first lane whose end is past it
-#pragma unroll
-            for (int step = WAVE / 2; step; step /= 2)
-                if ((uint32_t)__shfl((int)end, at + step - 1, WAVE) <= p) at += step;
-            at = at < WAVE ? at : WAVE - 1;
-            const uint32_t e = (uint32_t)__shfl((int)end, at, WAVE), n = (uint32_t)__shfl((int)pages, at, WAVE),
-                           f = (uint32_t)__shfl((int)from, at, WAVE);
-            if (p < all) any |= a.table[(uint64_t)(s0 + at) * a.table_stride + f + (p - (e - n))] >= a.kv.n_pages;
-        }
-    }
-    if (any) wrong = DEV_ERR_BAD_LAYOUT;
-    __syncthreads();
-    if (threadIdx.x == 0) *a.status = wrong;
-}
-
-// slot of row t of sequence s, negative if it has none: by the length as it is, so that one above
-// max_kv moves no row to another's slot
-__device__ __forceinline__ int64_t slot_of_row(const AppendArgs &a, uint32_t s, const Seq &q, uint32_t t) {
-    const int64_t slot = (int64_t)a.kv_len[s] - q.rows + (t - q.first);
-    return slot < (int64_t)a.max_kv ? slot : -1;
-}
-
-__device__ __forceinline__ float to_float(uint32_t bits, bool bf16) {
-    if (bf16) return __uint_as_float(bits << 16);
-    return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    const int any = __syncthreads_or(chunks_bad(a, 0xFFFFFFFFu));
+    if (threadIdx.x == 0) *a.status = any ? DEV_ERR_BAD_LAYOUT : 0;
 }
 
 // four elements (two words) to four codes
 template <bool BF16>
 __device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b, float scale) {
-    float x[4] = {to_float(a & 0xFFFF, BF16), to_float(a >> 16, BF16), to_float(b & 0xFFFF, BF16), to_float(b >> 16, BF16)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float y = x[i] / scale;
-        x[i] = y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
-    }
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
-    return (uint32_t)w;
+    return to_e4m3(to_float(a & 0xFFFF, BF16), to_float(a >> 16, BF16), to_float(b & 0xFFFF, BF16), to_float(b >> 16, BF16), scale);
 }
 
 // A wave a row, so that the row's chain of loads is all there is and its addresses are
@@ -137,7 +109,7 @@ __global__ __launch_bounds__(256) void append_few_kernel(AppendArgs a) {
     bool bad;
     const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
     if (t < q.first || t - q.first >= q.rows) return;
-    const int64_t slot = slot_of_row(a, s, q, t);
+    const int64_t slot = slot_of_row(a.kv_len, a.max_kv, s, q, t);
     if (slot < 0) return;
     const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;
     const uint32_t page = a.table[(uint64_t)s * a.table_stride + at];
@@ -161,22 +133,6 @@ __global__ __launch_bounds__(256) void append_few_kernel(AppendArgs a) {
                                                   to_e4m3<MODE == 1>(y1.x, y1.y, vs), to_e4m3<MODE == 1>(y1.z, y1.w, vs));
         }
     }
-}
-
-// sequence of chunk row t, by a whole wave: the first that ends past it (or the last one)
-__device__ __forceinline__ uint32_t wave_seq_of(const uint32_t *__restrict__ q_off, uint32_t n_seqs, uint32_t t) {
-    const uint32_t lane = threadIdx.x & (WAVE - 1);
-    uint32_t lo = 0, n = n_seqs;   // one of lo .. lo + n - 1
-    while (n > 1) {
-        const uint32_t step = (n + WAVE - 1) / WAVE;
-        const bool in = lane * step < n;
-        const uint32_t end = in ? q_off[lo + min((lane + 1) * step, n)] : 0;
-        const uint32_t past = min((uint32_t)__popcll(ballot(in && end <= t)) * step, n - 1);
-        lo += past;
-        n = min(step, n - past);
-        if (step == 1) break;
-    }
-    return lo;
 }
 
 // Four rows to a wave, whose lanes take the 16-byte pieces of their cache entries, so that
@@ -209,7 +165,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             if (s + 1 < a.n_seqs && a.q_off[s + 1] <= t) s += 1 + seq_of(a.q_off + s + 1, a.n_seqs - s - 1, t);
             bool bad;
             const Seq q = load_seq(a.q_off, a.kv_len, s, a.n_rows, a.max_kv, &bad);
-            const int64_t slot = slot_of_row(a, s, q, t);
+            const int64_t slot = slot_of_row(a.kv_len, a.max_kv, s, q, t);
             there[u] = p < rows * a.pieces && t >= q.first && t - q.first < q.rows && slot >= 0;
             if (!there[u]) continue;
             const uint32_t at = a.kv.by_page.div((uint32_t)slot), off = (uint32_t)slot - at * a.kv.page;
@@ -553,6 +509,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t g
         const uint4 x = *(const uint4 *)(a.kv.k + src), y = *(const uint4 *)(a.kv.v + src);
         *(uint4 *)(a.kv.k + dst) = x;
         *(uint4 *)(a.kv.v + dst) = y;
+        if (a.kv.k_exp) {   // 16 bytes of 4-bit codes are a block
+            a.kv.k_exp[dst / 16] = a.kv.k_exp[src / 16];
+            a.kv.v_exp[dst / 16] = a.kv.v_exp[src / 16];
+        }
     }
 }
 
@@ -598,13 +558,13 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     const pc_status ok = kv_view(cache, &a.kv);
     if (ok != PC_OK) return ok;
     if (dtype != PC_BF16 && dtype != PC_F16) return PC_ERR_INVALID;
-    if (cache->dtype != dtype && cache->dtype != PC_FP8_E4M3) return PC_ERR_INVALID;
-    const bool f8 = cache->dtype == PC_FP8_E4M3;
-    a.by_head = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
+    const bool f8 = cache->dtype == PC_FP8_E4M3, f4 = cache->dtype == PC_FP4_E2M1;
+    if (cache->dtype != dtype && !f8 && !f4) return PC_ERR_INVALID;
+    a.by_head = fast_div((uint32_t)(bytes_of(cache->dtype, a.kv.dim) / 16));
     a.pieces = a.by_head.d * a.kv.n_kv;
     a.by_token = fast_div(a.pieces);
     const bool many = append_many(n_rows, a.pieces, f8);
-    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u || !launch_fits(append_groups(n_rows, many), 256))
+    if (n_seqs >= 0x80000000u || n_rows >= 0x80000000u || max_kv > 0x7FFF0000u || (!f4 && !launch_fits(append_groups(n_rows, many), 256)))
         return PC_ERR_TOO_LARGE;
     if (max_kv > table_stride * a.kv.page) return PC_ERR_INVALID;
     if (!kv_len || !q_off || (max_kv && !page_table) || (n_rows && (!k || !v))) return PC_ERR_INVALID;
@@ -628,6 +588,9 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
     a.v_row = v_stride_row * 2;
     a.v_head = v_stride_head * 2;
     a.status = (int32_t *)ws;
+    if (f4)
+        return append_turned(a, cache->dtype, Entries{k, a.k_row, a.k_head}, Entries{v, a.v_row, a.v_head}, dtype, Turn{}, Layout::PAIRS,
+                             Queries{}, a.status, st);
     if (!f8) return append_run<0>(a, many, st);
     return dtype == PC_BF16 ? append_run<1>(a, many, st) : append_run<2>(a, many, st);
 }
@@ -676,7 +639,7 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     a.kept = kept;
     a.new_len = new_len;
     a.weight_out = weight_out;
-    a.by_piece = fast_div((uint32_t)(a.kv.dim * type_size(cache->dtype) / 16));
+    a.by_piece = fast_div((uint32_t)(bytes_of(cache->dtype, a.kv.dim) / 16));
     if (evict_split(max_kv)) {
         const dim3 grid((unsigned)b.all);
         PC_LAUNCH(K_KV_EVICT_SELECT, evict_split_kernel<0>, grid, dim3(SELECT_THREADS), 0, st, a, b);

@@ -23,6 +23,7 @@ LIB_PATH = os.path.join(HERE, "_lib", "libpc.so")
 NONE = 0xFFFFFFFF
 DEEPEST_FIRST = 1   # PC_HASH_DEEPEST_FIRST
 PREV_ONLY = 2       # PC_PREV_ONLY
+ROPE_INTERLEAVED, ROPE_TRANSPOSE = 1, 2   # PC_ROPE_INTERLEAVED, PC_ROPE_TRANSPOSE
 
 _lib = None
 
@@ -42,6 +43,11 @@ class _KvCache(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("stride_page", _u64),
                 ("stride_head", _u64), ("stride_slot", _u64), ("dtype", _u32), ("n_pages", _u32), ("page_size", _u32),
                 ("n_kv_heads", _u32), ("head_dim", _u32)]
+
+
+class _Rotation(ctypes.Structure):
+    """pc_rotation"""
+    _fields_ = [("table", _vp), ("pos", _vp), ("n_pos", _u32), ("rot_dim", _u32), ("flags", _u32)]
 
 
 def lib():
@@ -121,6 +127,17 @@ def lib():
     L.pc_kv_append.restype = _st
     L.pc_kv_append.argtypes = [_vp, _vp, _u64, _vp, _vp, _u32, _u32, _u32, _vp, _u64, _u64, _vp, _u64, _u64, _u32,
                                _vp, _sz, _vp]
+    L.pc_rope_table.restype = _st
+    L.pc_rope_table.argtypes = [_vp, _u32, _u64, _u64, ctypes.c_double, _vp, _vp]
+    L.pc_rope_ws.restype = _sz
+    L.pc_rope_ws.argtypes = []
+    L.pc_rope.restype = _st
+    L.pc_rope.argtypes = [_vp, _vp, _u64, _u64, _vp, _u64, _u64, _u32, _u32, _u32, _u32, _vp, _sz, _vp]
+    L.pc_kv_append_rope_ws.restype = _sz
+    L.pc_kv_append_rope_ws.argtypes = []
+    L.pc_kv_append_rope.restype = _st
+    L.pc_kv_append_rope.argtypes = [_vp, _vp, _u64, _vp, _vp, _u32, _u32, _u32, _vp, _vp, _u64, _u64, _vp, _u64, _u64,
+                                    _vp, _u64, _u64, _vp, _u64, _u64, _u32, _u32, _vp, _sz, _vp]
     L.pc_attn_paged_ws.restype = _sz
     L.pc_attn_paged_ws.argtypes = [_u32, _u32, _u32, _u32, _u32, _u32, _u32, ctypes.c_int]
     L.pc_attn_paged.restype = _st
@@ -509,7 +526,8 @@ def belady(nxt: torch.Tensor, caps: torch.Tensor, depth: Optional[torch.Tensor] 
 
 # ------------------------------------------------------------- paged cache
 
-_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}   # PC_BF16, PC_F16, PC_FP8_E4M3
+# PC_BF16, PC_F16, PC_FP8_E4M3, PC_FP4_E2M1
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, torch.float4_e2m1fn_x2: 3}
 _INTS = (torch.int32, torch.uint32)
 _MAX_KV = 0x7FFF0000
 
@@ -569,7 +587,10 @@ class PagedCache:
     """A paged cache of KV blocks (``pc_kv_cache``) over two tensors [page, head,
     slot, head_dim] of one type and one set of strides, head_dim contiguous: pages
     kept as [page, slot, head, head_dim] go in as ``x.transpose(1, 2)``.  bfloat16,
-    float16, or float8_e4m3fn with ``k_scale`` and ``v_scale`` (float32, one per head).
+    float16, float8_e4m3fn with ``k_scale`` and ``v_scale`` (float32, one per head), or
+    float4_e2m1fn_x2 ([page, head, slot, head_dim / 2], two codes an element) with scales
+    [page, head, slot, head_dim / 32] of float8_e8m0fnu (or uint8, its bits) whose strides are
+    a sixteenth of the codes'; bytes of a plain buffer go in as ``x.view(torch.float4_e2m1fn_x2)``.
     The calls on it have no backward pass and refuse tensors that require a gradient
     (outside of ``torch.no_grad()``)."""
 
@@ -577,25 +598,43 @@ class PagedCache:
                  v_scale: Optional[torch.Tensor] = None):
         dtype, shape, stride = _DTYPES.get(k.dtype), k.shape, k.stride()
         if len(shape) != 4 or v.shape != shape or v.dtype != k.dtype or dtype is None:
-            raise PcError("expected two tensors [page, head, slot, head_dim] of bfloat16, float16 or float8_e4m3fn")
+            raise PcError("expected two tensors [page, head, slot, head_dim] of bfloat16, float16, float8_e4m3fn or "
+                          "float4_e2m1fn_x2")
         if not (k.is_cuda and v.is_cuda):
             raise PcError("expected a GPU tensor")
         if stride[3] != 1 or (v.stride() != stride and any(a != b for a, b, n in zip(stride, v.stride(), shape) if n > 1)):
             raise PcError("expected equal strides of k and v, head_dim contiguous")
-        if (k_scale is None) != (dtype != 2) or (v_scale is None) != (dtype != 2):
-            raise PcError("k_scale and v_scale go with float8_e4m3fn")
-        for x in (k_scale, v_scale):
-            if x is not None and (x.dtype != torch.float32 or x.shape != shape[1:2]):
-                raise PcError("expected one float32 scale per head")
+        if (k_scale is None) != (dtype < 2) or (v_scale is None) != (dtype < 2):
+            raise PcError("k_scale and v_scale go with float8_e4m3fn and float4_e2m1fn_x2")
+        if dtype == 3:
+            shape = shape[:3] + (2 * shape[3],)
+            stride = [2 * s if n > 1 else shape[3] for s, n in zip(stride[:3], shape)] + [1]
+            self._block_scales(k_scale, shape, stride, v_scale)
+        else:
+            for x in (k_scale, v_scale):
+                if x is not None and (x.dtype != torch.float32 or x.shape != shape[1:2]):
+                    raise PcError("expected one float32 scale per head")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self._grad = k.requires_grad or v.requires_grad or (
             k_scale is not None and (k_scale.requires_grad or v_scale.requires_grad))
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
         if 1 in shape:   # the stride of a dimension of one is anything
             stride = [s if n > 1 else self.head_dim for s, n in zip(stride, shape)]
-        self._c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), stride[0], stride[1], stride[2],
-                           dtype, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
+        scales = [x.data_ptr() for x in (k_scale, v_scale)] if dtype == 3 else [_ptr(k_scale), _ptr(v_scale)]
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), *scales, stride[0], stride[1], stride[2], dtype,
+                           self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
         self._at = ctypes.addressof(self._c)
+
+    @staticmethod
+    def _block_scales(k_scale, shape, stride, v_scale):
+        """Those of element i .. i + 31 lie at i / 32 (pc_kv_cache), so the strides follow from the codes'."""
+        blocks = shape[:3] + (shape[3] // 32,)
+        for x in (k_scale, v_scale):
+            if x.dtype not in (torch.uint8, torch.float8_e8m0fnu) or x.shape != blocks or not x.is_cuda:
+                raise PcError("expected scales %s of float8_e8m0fnu or uint8 on the GPU" % list(blocks))
+            if (blocks[3] > 1 and x.stride(3) != 1) or any(
+                    32 * a != b for a, b, n in zip(x.stride(), stride, shape[:3]) if n > 1):
+                raise PcError("scales: expected a sixteenth of the codes' strides")
 
 
 def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, q_off: torch.Tensor,
@@ -619,6 +658,124 @@ def kv_append(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor,
     check(L.pc_kv_append(cache._at, table, stride, _index(kv_len, "kv_len", n_seqs), _index(q_off, "q_off", n_seqs + 1),
                          n_seqs, shape[0], max_kv, ka, kr, kh, va, vr, vh, dtype, _ptr(ws), ws.numel(), _stream_of(k)))
     return ws
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                     trained: int = 0, slow: float = 1.0, fast: float = 32.0) -> np.ndarray:
+    """Angles a position of the rot_dim / 2 pairs of dimensions, float64 on the host:
+    f_i = base^(-2 i / rot_dim).  For contexts ``factor`` times longer than trained on, ``scaling``:
+    "linear"  f_i / factor (positions interpolated; Chen et al. 2023);
+    "base"    the base grown by factor^(rot_dim / (rot_dim - 2)), which divides the last f_i by factor and keeps the first;
+    "ramp"    by parts (Peng et al. 2023): a pair that makes t = ``trained`` f_i / (2 pi) turns over the context that was
+              trained keeps its f_i where t >= fast, takes f_i / factor where t <= slow, and in between
+              (1 - g) f_i / factor + g f_i with g = (t - slow) / (fast - slow).
+    """
+    if rot_dim < 2 or rot_dim % 2:
+        raise PcError("rot_dim: expected an even number of dimensions")
+    if not (np.isfinite(base) and base > 0 and np.isfinite(factor) and factor > 0):
+        raise PcError("base and factor: expected numbers above 0")
+    if scaling not in (None, "none", "linear", "base", "ramp"):
+        raise PcError("scaling: expected none, linear, base or ramp")
+    if scaling == "base" and rot_dim > 2:
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    freq = float(base) ** (np.arange(0, rot_dim, 2, dtype=np.float64) / -rot_dim)
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "ramp":
+        if not (trained > 0 and fast > slow):
+            raise PcError("ramp: expected the trained length, and slow < fast")
+        keep = np.clip((trained * freq / (2 * np.pi) - slow) / (fast - slow), 0, 1)
+        freq = (1 - keep) * freq / factor + keep * freq
+    return freq
+
+
+def rope_table(freq, n_pos: int, first: int = 0, magnitude: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pc_rope_table: [n_pos, pairs, 2] float32, ``magnitude`` times the cosine and sine of
+    the angles (first + p) freq[i].  ``freq`` is a float64 array on the host."""
+    L = lib()
+    freq = np.ascontiguousarray(freq, dtype=np.float64)
+    if freq.ndim != 1 or not 0 <= n_pos < NONE or not 0 <= first < NONE:
+        raise PcError("expected one frequency a pair, and positions below 2^32 - 1")
+    shape = (n_pos, freq.size, 2)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=_dev())
+    elif out.dtype != torch.float32 or out.shape != shape:
+        raise PcError("out: expected %s float32" % list(shape))
+    check(L.pc_rope_table(freq.ctypes.data, freq.size, first, n_pos, magnitude, _ptr(out), _stream_of(out)))
+    return out
+
+
+def _rotation(table: torch.Tensor, pos: Optional[torch.Tensor], n_rows: int, flags: int) -> _Rotation:
+    if table.dtype != torch.float32 or len(table.shape) != 3 or table.shape[2] != 2 or table.shape[0] >= NONE:
+        raise PcError("table: expected [positions, pairs, 2] float32")
+    return _Rotation(_ptr(table), None if pos is None else _index(pos, "pos", n_rows), table.shape[0], 2 * table.shape[1], flags)
+
+
+def rope(x: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None, interleaved: bool = False,
+         transpose: bool = False, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """pc_rope: rows ``x`` [rows, head, head_dim] turned by the angles of their positions (``pos``, 32-bit integers;
+    their numbers if not given), in the first 2 * pairs dimensions of every head.  ``transpose`` turns back: it
+    takes the gradient of the result to that of ``x``.  ``out`` may be ``x``.  Returns (out, ws)."""
+    L = lib()
+    if x.requires_grad or table.requires_grad:
+        _no_gradient()
+    dtype, shape = _DTYPES.get(x.dtype), x.shape
+    if len(shape) != 3 or dtype is None:
+        raise PcError("expected x as [rows, heads, head_dim] of bfloat16 or float16")
+    xa, xr, xh = _rows(x, "x", shape)
+    if out is None:
+        out = x.new_empty(shape)
+        oa, o_r, oh = out.data_ptr(), shape[1] * shape[2], shape[2]
+    else:
+        if out.dtype != x.dtype:
+            raise PcError("out: expected x's type")
+        oa, o_r, oh = _rows(out, "out", shape)
+    turn = _rotation(table, pos, shape[0], (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_TRANSPOSE if transpose else 0))
+    if ws is None:
+        ws = _scratch(L.pc_rope_ws(), x)
+    check(L.pc_rope(ctypes.addressof(turn), xa, xr, xh, oa, o_r, oh, dtype, shape[0], shape[1], shape[2], _ptr(ws), ws.numel(),
+                    _stream_of(x)))
+    return out, ws
+
+
+def kv_append_rope(cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor, q_off: torch.Tensor,
+                   k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                   interleaved: bool = False, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                   max_kv: Optional[int] = None, ws: Optional[torch.Tensor] = None):
+    """pc_kv_append_rope: ``kv_append`` of keys turned by the angles of their positions (``pos``, 32-bit integers, one
+    per row; their slots if not given), and in the same launch the rows' queries ``q`` [rows, query head, head_dim],
+    to ``q_out`` (which may be ``q``).  Returns (q_out or None, ws)."""
+    L = lib()
+    if k.requires_grad or v.requires_grad or table.requires_grad or cache._grad or (q is not None and q.requires_grad):
+        _no_gradient()
+    n_seqs = kv_len.shape[0]
+    pages, stride = _table(page_table, "page_table", n_seqs)
+    max_kv = _room(page_table, cache, max_kv)
+    dtype = _DTYPES.get(k.dtype)
+    if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise PcError("expected q, k and v of one type, bfloat16 or float16")
+    shape = (k.shape[0], cache.n_kv_heads, cache.head_dim)
+    ka, kr, kh = _rows(k, "k", shape)
+    va, vr, vh = _rows(v, "v", shape)
+    qa = qr = qh = oa = o_r = oh = heads = 0
+    if q is not None:
+        heads = q.shape[1] if len(q.shape) == 3 else 0
+        q_shape = (shape[0], heads, shape[2])
+        qa, qr, qh = _rows(q, "q", q_shape)
+        if q_out is None:
+            q_out = q.new_empty(q_shape)
+        elif q_out.dtype != q.dtype:
+            raise PcError("q_out: expected q's type")
+        oa, o_r, oh = _rows(q_out, "q_out", q_shape)
+    elif q_out is not None:
+        raise PcError("q_out goes with q")
+    turn = _rotation(table, pos, shape[0], ROPE_INTERLEAVED if interleaved else 0)
+    if ws is None:
+        ws = _scratch(L.pc_kv_append_rope_ws(), k)
+    check(L.pc_kv_append_rope(cache._at, pages, stride, _index(kv_len, "kv_len", n_seqs), _index(q_off, "q_off", n_seqs + 1),
+                              n_seqs, shape[0], max_kv, ctypes.addressof(turn), ka, kr, kh, va, vr, vh, qa or None, qr, qh,
+                              oa or None, o_r, oh, heads, dtype, _ptr(ws), ws.numel(), _stream_of(k)))
+    return q_out, ws
 
 
 def attn_paged(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, kv_len: torch.Tensor,

@@ -2,6 +2,8 @@
 // products, the work list, tiles of keys and values.  Not part of the ABI.
 #pragma once
 
+#include <type_traits>
+
 #include "pc_kv.h"
 
 namespace pc {
@@ -144,16 +146,15 @@ struct ValueAt {
         }
     }
 };
-// Where this lane finds its key (or query row) lane % 32 of a tile, step i of its dimensions: runs of
-// 16 of them in turn with the other half of the wave, or of 32 (a block of 4-bit codes a lane).
-template <int D, bool BLOCKS = false>
+// Where this lane finds its key (or query row) lane % 32 of a tile, step i of its dimensions.
+template <int D>
 struct RowAt {
     uint32_t at[D == 64 ? 4 : 8];
     __device__ __forceinline__ RowAt() {
         const uint32_t lane = threadIdx.x & (WAVE - 1);
 #pragma unroll
         for (uint32_t i = 0; i < (D == 64 ? 4 : 8); ++i)
-            at[i] = piece_at<D>(lane % 32, BLOCKS ? 8 * (i / 4) + 4 * (lane / 32) + i % 4 : 4 * (i / 2) + 2 * (lane / 32) + i % 2);
+            at[i] = piece_at<D>(lane % 32, 4 * (i / 2) + 2 * (lane / 32) + i % 2);
     }
     __device__ __forceinline__ uint4 read(const char *tile, int i) const {
         return *(const uint4 *)(tile + at[i % (D == 64 ? 4 : 8)] + i / 8 * 256);
@@ -183,6 +184,7 @@ struct AttnArgs {
     uint32_t target;             // items wanted
     uint32_t least;              // tiles of an item, at least
     uint32_t cut_first;          // the ranges of sequences that are cut come first: what is left for the end is smaller
+    uint32_t even;               // a sequence's ranges are of one length, not all but the last as long as they may be
     uint32_t row_tile, key_tile; // rows, keys
     uint32_t slots;              // partial results that fit
     uint32_t slot_rows;
@@ -267,18 +269,22 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
 #pragma unroll
     for (int step = 1; step < WAVE; step *= 2) tiles += __shfl_xor((unsigned long long)tiles, step, WAVE);
     const uint64_t len = (tiles * a.kv.n_kv + a.target - 1) / a.target;
-    it.length = uniform(len > a.least ? (uint32_t)(len < 0x7FFFFFFFu ? len : 0x7FFFFFFFu) : a.least);
+    const uint32_t longest = uniform(len > a.least ? (uint32_t)(len < 0x7FFFFFFFu ? len : 0x7FFFFFFFu) : a.least);
     uint64_t base = 0, slot = 0;
     const int classes = BY != By::SEQ && a.cut_first ? 2 : 1;
 #pragma unroll 1
     for (int whole = 0; whole < classes; ++whole) {
         for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += WAVE) {
             const uint32_t s = s0 + lane;
-            uint32_t items = 0, splits = 1, count = 0;
+            uint32_t items = 0, splits = 1, count = 0, length = longest;
             if (s < a.n_seqs) {
                 if (a.n_seqs > WAVE) h = shape_of(a, s);
-                splits = (h.key_tiles + it.length - 1) / it.length;
+                splits = (h.key_tiles + length - 1) / length;
                 splits = splits ? splits : 1;
+                if (a.even && splits > 1) {
+                    length = (h.key_tiles + splits - 1) / splits;
+                    splits = (h.key_tiles + length - 1) / length;
+                }
                 const uint64_t n = (uint64_t)h.row_tiles * splits * a.kv.n_kv;
                 items = n < (1u << 25) ? (uint32_t)n : 1u << 25;
                 if (classes == 1 || (splits == 1) == (whole == 1)) count = BY == By::ITEM ? items : h.row_tiles * a.kv.n_kv;
@@ -293,6 +299,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
                 it.there = true;
                 it.seq = s0 + at;
                 it.splits = from_lane(splits, at);
+                it.length = from_lane(length, at);
                 it.shape.q.first = from_lane(h.q.first, at);
                 it.shape.q.rows = from_lane(h.q.rows, at);
                 it.shape.q.len = from_lane(h.q.len, at);
@@ -436,5 +443,42 @@ __device__ __forceinline__ float score_factor(const AttnArgs &a, uint32_t h, uin
     *flip = c < 0.f ? 0x80008000u : 0u;
     return *zero ? 1.f : fabsf(c);
 }
+
+// ------------------------------------------------------------ keys and values
+
+// address of a slot's entry in `base`, the page taken as is (it is below n_pages)
+__device__ __forceinline__ uint64_t entry_at(const KvView &kv, uint32_t page, uint32_t off, uint32_t head) {
+    return page * kv.sp + off * kv.st + head * kv.sh;
+}
+// a table entry that does not fit reads page 0 (the join reports it)
+__device__ __forceinline__ uint32_t page_of(const KvView &kv, uint32_t entry) { return entry < kv.n_pages ? entry : 0; }
+
+// x with the elements that are not finite zeroed; *any is set if there are any
+template <class T>
+__device__ __forceinline__ uint32_t drop_not_finite(uint32_t w, bool *any) {
+    const bool lo = (w & T::EXPONENT) == T::EXPONENT, hi = (w >> 16 & T::EXPONENT) == T::EXPONENT;
+    *any |= lo | hi;
+    return (lo ? 0 : w & 0xFFFFu) | (hi ? 0 : w & 0xFFFF0000u);
+}
+template <class T>
+__device__ __forceinline__ uint4 drop_not_finite(uint4 x, bool *any) {
+    return make_uint4(drop_not_finite<T>(x.x, any), drop_not_finite<T>(x.y, any), drop_not_finite<T>(x.z, any),
+                      drop_not_finite<T>(x.w, any));
+}
+
+// log2 of a row's sum of exponentials, from its maximum and its sum relative to that.  A sum of
+// zero is a row that sees nothing (or scores of -inf alone); the maximum does not say so:
+// it passes over NaN, which is in the sum.
+template <class T>
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l == 0.f ? MINUS_INF : m + __log2f(l) - T::TOP;
+}
+
+// ------------------------------------------------------------------ 4 bits
+
+// The path for few rows over a cache in 4 bits (pc_attn4.hip): max_rows of a sequence and head; scores are kept
+// where a.scores is there.
+uint32_t rows4_resident(uint32_t dim, uint32_t max_rows);   // workgroups that the chip holds at once
+pc_status attn_rows4(const AttnArgs &a, bool bf16, uint32_t dim, uint32_t max_rows, dim3 items, hipStream_t st);
 
 }  // namespace pc

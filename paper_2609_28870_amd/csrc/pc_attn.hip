@@ -9,28 +9,6 @@
 
 namespace pc {
 
-// ------------------------------------------------------------ keys and values
-
-// address of a slot's entry in `base`, the page taken as is (it is below n_pages)
-__device__ __forceinline__ uint64_t entry_at(const KvView &kv, uint32_t page, uint32_t off, uint32_t head) {
-    return page * kv.sp + off * kv.st + head * kv.sh;
-}
-// a table entry that does not fit reads page 0 (the join reports it)
-__device__ __forceinline__ uint32_t page_of(const KvView &kv, uint32_t entry) { return entry < kv.n_pages ? entry : 0; }
-
-// x with the elements that are not finite zeroed; *any is set if there are any
-template <class T>
-__device__ __forceinline__ uint32_t drop_not_finite(uint32_t w, bool *any) {
-    const bool lo = (w & T::EXPONENT) == T::EXPONENT, hi = (w >> 16 & T::EXPONENT) == T::EXPONENT;
-    *any |= lo | hi;
-    return (lo ? 0 : w & 0xFFFFu) | (hi ? 0 : w & 0xFFFF0000u);
-}
-template <class T>
-__device__ __forceinline__ uint4 drop_not_finite(uint4 x, bool *any) {
-    return make_uint4(drop_not_finite<T>(x.x, any), drop_not_finite<T>(x.y, any), drop_not_finite<T>(x.z, any),
-                      drop_not_finite<T>(x.w, any));
-}
-
 // Values that are not finite, in tiles whose keys some rows see and some do not: the
 // matrix product would carry 0 * inf = NaN to rows that do not see the key.  Such a
 // tile is worked on without them, and where there were any they are added here, after
@@ -60,6 +38,26 @@ __device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs
     s = sum_of_halves(s);
     const float p = exp2_fast(fmaf(s, c, T::TOP - state.m * c));
     const bool visible = (int32_t)key >= first && (int32_t)key <= last;
+    if constexpr (H == Held::E2M1) {
+        // four codes are two bytes, and a block has one scale
+        const char *x = a.kv.v + entry + 2 * half;
+        const uint8_t *exponents = a.kv.v_exp + entry / 16;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            if (32u * b >= a.kv.dim) break;
+            const float scale = scale_of(exponents[b]);
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const uint32_t w = *(const uint16_t *)(x + 16 * b + r);
+                const uint32_t lo = T::template from_e2m1<0>(w, scale), hi = T::template from_e2m1<1>(w, scale);
+                const float y[4] = {T::value(lo & 0xFFFF), T::value(lo >> 16), T::value(hi & 0xFFFF), T::value(hi >> 16)};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) state.o[b][r + i] += visible && !(fabsf(y[i]) < __builtin_inff()) ? p * y[i] : 0.f;
+                __asm__ volatile("" ::: "memory");   // few of the loads at once: the registers are full
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -69,14 +67,6 @@ __device__ __forceinline__ void add_not_finite(Rows<T, D> &state, const AttnArgs
             state.o[b][r] += visible && !(fabsf(x) < __builtin_inff()) ? p * x : 0.f;
             if (r % 4 == 3) __asm__ volatile("" ::: "memory");   // few of the loads at once: the registers are full
         }
-}
-
-// log2 of a row's sum of exponentials, from its maximum and its sum relative to that.  A sum of
-// zero is a row that sees nothing (or scores of -inf alone); the maximum does not say so:
-// it passes over NaN, which is in the sum.
-template <class T>
-__device__ __forceinline__ float log_sum(float m, float l) {
-    return l == 0.f ? MINUS_INF : m + __log2f(l) - T::TOP;
 }
 
 // A row's result: whole (its sequence is one item long), or a part for the join.
@@ -126,10 +116,8 @@ __device__ __forceinline__ void write_rows(const AttnArgs &a, const Item &it, co
 // times); one token over 1,537 keys 11 us, a chain of dependent loads.
 template <class T, Held H, int D, bool FULL, bool WEIGHTS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a) {
-    constexpr bool F8 = H == Held::E4M3, F4 = H == Held::E2M1;
-    constexpr int PIECES = held_bytes<H>(D) / 32;   // 16 bytes, of one lane's half of a key
-    constexpr int STEPS = D / 16 / PIECES;          // of the product, that a piece serves
-    constexpr int WORDS = (D + 127) / 128;          // of a key's scales (4-bit)
+    constexpr bool F8 = H == Held::E4M3;
+    constexpr int PIECES = F8 ? D / 32 : D / 16;   // 16 bytes, of one lane's half of a key
     __shared__ __attribute__((aligned(16))) char tiles[4 * 32 * D * 2];
     __shared__ __attribute__((aligned(16))) char queries[32 * D * 2];   // the same for all waves
     __shared__ float2 join_ml[2][64];
@@ -170,35 +158,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         entry = table[p];
     };
     auto load = [&](const char *base, uint4 (&x)[PIECES]) {
-        const char *p = base + at + half * (H == Held::SAME ? 32 : 16);
+        const char *p = base + at + half * (F8 ? 16 : 32);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t o = H == Held::SAME ? 2 * dim_of_step(i, 0) : 32 * i;
+            const uint32_t o = F8 ? 32 * i : 2 * dim_of_step(i, 0);
             // past the head's dimensions: its first ones
-            if (FULL || o + half * (H == Held::SAME ? 32 : 16) < held_bytes<H>(a.kv.dim)) x[i] = *(const uint4 *)(p + o);
+            if (FULL || o + half * (F8 ? 16 : 32) < a.kv.dim * (F8 ? 1 : 2)) x[i] = *(const uint4 *)(p + o);
             else x[i] = *(const uint4 *)(base + at);
         }
     };
-    // Scales of the key at hand: this lane's blocks (every other one) are bytes 0 and 2 of a word.
-    uint32_t ke[WORDS], ve[WORDS];
-    auto load_scales = [&](const uint8_t *base, uint32_t (&e)[WORDS]) {
-        if (!F4) return;
-        const uint8_t *p = base + at / 16;
-        if (FULL) {
-            uint32_t x[WORDS] = {};
-            __builtin_memcpy(x, p, D / 32);
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) e[i] = x[i] >> 8 * half;
-        } else {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) e[i] = 0;
-#pragma unroll
-            for (int i = 0; i < (F4 ? PIECES : 0); ++i)
-                if (2 * i + half < a.kv.dim / 32) e[i / 2] |= (uint32_t)p[2 * i + half] << 16 * (i % 2);
-        }
-    };
-    auto scale = [&](const uint32_t (&e)[WORDS], int i) { return scale_of(e[i / 2 % WORDS] >> 16 * (i % 2) & 0xFF); };
-    auto word = [](uint4 x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
     if (t < t_end) look_up(t);
     uint4 q[D / 64];
 #pragma unroll
@@ -211,9 +179,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
     if (t < t_end) {
         at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
         load(a.kv.k, k);
-        load_scales(a.kv.k_exp, ke);
         load(a.kv.v, v);
-        load_scales(a.kv.v_exp, ve);
         if (t + 4 < t_end) look_up(t + 4);
     }
     sign_query<T>(q, flip, zero);
@@ -222,7 +188,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         *(uint4 *)(queries + piece_at<D>((threadIdx.x + 256 * i) / (D / 8), threadIdx.x % (D / 8))) = q[i];
     __syncthreads();
     bool odd = false;   // a value that is not finite was left out of a tile
-    const RowAt<D, F4> q_at;
+    const RowAt<D> q_at;
     const ValueAt<D> v_at;
     const float slack = slack_of<T>(c);
     auto query = [&](int i) { return q_at.read(queries, i); };
@@ -234,37 +200,30 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         if (!FULL) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                if ((F4 ? 64 * i + 32 * half : F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
+                if ((F8 ? 32 * i + 16 * half : dim_of_step(i, half)) >= a.kv.dim) k[i] = make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            const uint4 &piece = k[i / STEPS];
-            if (F4) {
-                s[0] = T::mfma(expand<T>(word(piece, i % 4), scale(ke, i / STEPS)), query(i), i ? s[0] : f32x16(0.f));
-            } else if (F8) {
+            if (F8) {
                 uint4 x, y;
-                expand<T>(piece, &x, &y);
+                expand<T>(k[i / 2], &x, &y);
                 s[0] = T::mfma(i % 2 ? y : x, query(i), i ? s[0] : f32x16(0.f));
             } else {
-                s[0] = T::mfma(piece, query(i), i ? s[0] : f32x16(0.f));
+                s[0] = T::mfma(k[i % PIECES], query(i), i ? s[0] : f32x16(0.f));
             }
         }
         if (more) {
             at = entry_at(a.kv, page_of(a.kv, entry), off, it.head);
             load(a.kv.k, k);
-            load_scales(a.kv.k_exp, ke);
         }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t n = F4 ? 8 * i + 4 * half : F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
+            const uint32_t n = F8 ? 4 * i + 2 * half : dim_of_step(i, half) / 8;
             auto put = [&](uint4 x, int e) {
                 if (!full) x = drop_not_finite<T>(x, &odd);
                 *(uint4 *)(tile + piece_at<D>(col, n + e)) = x;
             };
-            if (F4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) put(expand<T>(word(v[i], e), scale(ve, i)), e);
-            } else if (F8) {
+            if (F8) {
                 uint4 x, y;
                 expand<T>(v[i], &x, &y);
                 put(x, 0);
@@ -275,7 +234,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void rows_kernel(AttnArgs a)
         }
         if (more) {
             load(a.kv.v, v);
-            load_scales(a.kv.v_exp, ve);
             if (t + 8 < t_end) look_up(t + 8);
         }
         if (!full) {
@@ -1050,8 +1008,13 @@ template <class T, Held H, int D, bool FULL>
 static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids &g, hipStream_t st) {
     const dim3 items((unsigned)g.items);
     if (p.few) {
-        if (p.scores) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, true>), items, dim3(256), 0, st, a);
-        else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, false>), items, dim3(256), 0, st, a);
+        if constexpr (H == Held::E2M1) {
+            const pc_status ok = attn_rows4(a, std::is_same<T, Bf16>::value, D, p.slot_rows, items, st);
+            if (ok != PC_OK) return ok;
+        } else {
+            if (p.scores) PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, true>), items, dim3(256), 0, st, a);
+            else PC_LAUNCH(K_ATTN_ROWS, (rows_kernel<T, H, D, FULL, false>), items, dim3(256), 0, st, a);
+        }
     } else if (p.wide) {
         constexpr int W = D == 128 ? CHUNK_WAVES_WIDE : CHUNK_WAVES;
         PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, H, D, FULL, W>), items, dim3(W * WAVE), 0, st, a);
@@ -1145,8 +1108,16 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.causal = flags & PC_ATTN_CAUSAL;
     a.window = window;
     a.by_16 = a.kv.page % 16 == 0 && a.kv.st < (1u << 24);
+    if (!p.scores) a.scores = nullptr;   // the workspace may have room for them all the same
     a.target = p.items;
     a.cut_first = p.ragged;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
+    a.even = cache->dtype == PC_FP4_E2M1 && p.few;
+    if (a.even) {
+        // one round of the chip, less the half range more that every sequence and head is likely to make
+        const uint32_t round = rows4_resident(p.dim, p.slot_rows), halves = (uint32_t)((uint64_t)n_seqs * a.kv.n_kv / 2 < round / 2
+                                                                                           ? n_seqs * a.kv.n_kv / 2 : round / 2);
+        a.target = round - halves;
+    }
     a.least = p.few ? ROWS_LEAST : CHUNK_LEAST * 64 / chunk_keys(p.dim);
     a.row_tile = p.row_tile;
     a.key_tile = p.few ? 32 : chunk_keys(p.dim);

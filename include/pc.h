@@ -558,8 +558,8 @@ typedef struct {
 } pc_rotation;
 
 /* table[p - first][i] = magnitude * (cos(p freq[i]), sin(p freq[i])), first <= p < first + n_pos.
- * The angle is a product in 64 bits, the result rounded to 32.
- *   freq       double[n_freq] in HOST memory, at most 1e6 in magnitude each: what a model stretches for
+ * The angle is the exact product, the result worked out in 64 bits and rounded to 32.
+ *   freq       double[n_freq] in HOST memory, at most 65536 in magnitude each: what a model stretches for
  *              contexts longer than it was trained on; read before the call returns
  *   n_freq     1 .. PC_MAX_HEAD_DIM / 2 (rot_dim / 2)
  *   magnitude  finite; first + n_pos below 2^32 - 1 */

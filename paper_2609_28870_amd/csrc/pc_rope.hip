@@ -55,35 +55,54 @@ struct Frequencies {
     double f[PC_MAX_HEAD_DIM / 2];
 };
 
-// The angle p f in 64 bits, less a multiple of pi/2 (the product with its two parts is exact in the
-// fused sums), and the series of sine and cosine on |r| <= pi/4 up to r^13 and r^14: both are off by less than
-// 3e-14 before they are rounded to 32 bits.  Bound by 64-bit arithmetic and the writes.
-__global__ __launch_bounds__(256) void rope_table_kernel(Frequencies freq, uint32_t half, FastDiv by_half, uint64_t first, uint64_t n_pos,
-                                                         uint32_t pos_of_group, double magnitude, float2 *__restrict__ out) {
-    const uint64_t p0 = (uint64_t)blockIdx.x * pos_of_group;
-    const uint32_t positions = (uint32_t)min((uint64_t)pos_of_group, n_pos - p0), pairs = positions * half;
-    for (uint32_t i = threadIdx.x; i < pairs; i += 256) {
-        const uint32_t p = by_half.div(i), d = i - p * half;
-        const double a = (double)(first + p0 + p) * freq.f[d];
-        const double n = rint(a * TWO_OVER_PI);
-        const double r = fma(-n, HALF_PI_REST, fma(-n, HALF_PI, a)), z = r * r;
-        double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
-        s = fma(s, z, -1.0 / 39916800.0);
-        s = fma(s, z, 1.0 / 362880.0);
-        s = fma(s, z, -1.0 / 5040.0);
-        s = fma(s, z, 1.0 / 120.0);
-        s = fma(s, z, -1.0 / 6.0);
-        s = fma(s * z, r, r);
-        c = fma(c, z, 1.0 / 479001600.0);
-        c = fma(c, z, -1.0 / 3628800.0);
-        c = fma(c, z, 1.0 / 40320.0);
-        c = fma(c, z, -1.0 / 720.0);
-        c = fma(c, z, 1.0 / 24.0);
-        c = fma(c, z, -0.5);
-        c = fma(c, z, 1.0);
-        const uint32_t quarter = (uint32_t)(long long)n;
-        const double x = (quarter & 1) ? s : c, y = (quarter & 1) ? c : s;
-        out[(p0 + p) * half + d] = make_float2((float)((((quarter + 1) & 2) ? -x : x) * magnitude), (float)(((quarter & 2) ? -y : y) * magnitude));
+// Cosine and sine of the product p f, p a whole number below 2^32: the product and what its rounding
+// leaves, less a multiple of pi/2 (exact in the fused sums), then their series on
+// |r| <= pi/4 up to r^14 and r^13, off by less than 3e-14.
+__device__ __forceinline__ double2 turn_by(double p, double f) {
+    const double a = p * f, n = rint(a * TWO_OVER_PI);
+    const double r = fma(-n, HALF_PI, a) + fma(-n, HALF_PI_REST, fma(p, f, -a)), z = r * r;
+    double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
+    s = fma(s, z, -1.0 / 39916800.0);
+    s = fma(s, z, 1.0 / 362880.0);
+    s = fma(s, z, -1.0 / 5040.0);
+    s = fma(s, z, 1.0 / 120.0);
+    s = fma(s, z, -1.0 / 6.0);
+    s = fma(s * z, r, r);
+    c = fma(c, z, 1.0 / 479001600.0);
+    c = fma(c, z, -1.0 / 3628800.0);
+    c = fma(c, z, 1.0 / 40320.0);
+    c = fma(c, z, -1.0 / 720.0);
+    c = fma(c, z, 1.0 / 24.0);
+    c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    // n modulo 4, which is below 2^51: from the bits of n + 1.5 * 2^52
+    const uint32_t quarter = (uint32_t)__double_as_longlong(n + 6755399441055744.0);
+    const double x = (quarter & 1) ? s : c, y = (quarter & 1) ? c : s;
+    return make_double2(((quarter + 1) & 2) ? -x : x, (quarter & 2) ? -y : y);
+}
+
+// A thread keeps its frequency over POSITIONS positions, `together` apart: the first angle and the
+// step are worked out, the others are the one turned by the other, four products in 64 bits, each off by
+// 2^-52 more.  (All of them worked out: 18.2 us for 131,072 positions of 64 pairs, bound by 64-bit arithmetic.)
+constexpr int POSITIONS = 16;
+__global__ __launch_bounds__(256) void rope_table_kernel(Frequencies freq, uint32_t half, uint32_t together, uint32_t first, uint32_t n_pos,
+                                                         double magnitude, float2 *__restrict__ out) {
+    const uint32_t at = threadIdx.x / half, d = threadIdx.x - at * half;
+    if (at >= together) return;
+    const double f = freq.f[d];
+    uint32_t p = blockIdx.x * (together * POSITIONS) + at;   // below 2^32: the last group starts inside the table
+    if (p >= n_pos) return;
+    const double2 step = turn_by(together, f);
+    double2 x = turn_by((double)first + (double)p, f);
+    x = make_double2(x.x * magnitude, x.y * magnitude);
+    float2 *to = out + (uint64_t)p * half + d;
+#pragma unroll
+    for (int i = 0; i < POSITIONS; ++i) {
+        *to = make_float2((float)x.x, (float)x.y);
+        if (n_pos - p <= together) return;
+        p += together;
+        to += together * half;
+        x = make_double2(fma(x.x, step.x, -(x.y * step.y)), fma(x.y, step.x, x.x * step.y));
     }
 }
 
@@ -524,16 +543,16 @@ pc_status pc_rope_table(const double *freq, uint32_t n_freq, uint64_t first, uin
     Frequencies f;
     for (uint32_t i = 0; i < PC_MAX_HEAD_DIM / 2; ++i) {
         f.f[i] = i < n_freq ? freq[i] : 0.0;
-        if (!(fabs(f.f[i]) <= 1e6)) return PC_ERR_INVALID;
+        if (!(fabs(f.f[i]) <= 65536.0)) return PC_ERR_INVALID;
     }
     if (n_pos > 0xFFFFFFFEull || first > 0xFFFFFFFEull || first + n_pos > 0xFFFFFFFEull) return PC_ERR_TOO_LARGE;
     if (n_pos && (!table || (uint64_t)(uintptr_t)table % 8)) return PC_ERR_INVALID;
     if (!n_pos) return PC_OK;
-    const uint32_t each = 1024 / n_freq;   // positions of a workgroup
-    const uint64_t groups = groups_of(n_pos, each);
+    const uint32_t together = 256 / n_freq;
+    const uint64_t groups = groups_of(n_pos, together * POSITIONS);
     if (!launch_fits(groups, 256)) return PC_ERR_TOO_LARGE;
-    PC_LAUNCH(K_ROPE_TABLE, rope_table_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, f, n_freq, fast_div(n_freq), first,
-              n_pos, each, magnitude, (float2 *)table);
+    PC_LAUNCH(K_ROPE_TABLE, rope_table_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, f, n_freq, together, (uint32_t)first,
+              (uint32_t)n_pos, magnitude, (float2 *)table);
     return PC_OK;
 }
 

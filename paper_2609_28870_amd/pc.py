@@ -12,6 +12,7 @@ raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -607,8 +608,8 @@ class PagedCache:
         if (k_scale is None) != (dtype < 2) or (v_scale is None) != (dtype < 2):
             raise PcError("k_scale and v_scale go with float8_e4m3fn and float4_e2m1fn_x2")
         if dtype == 3:
-            shape = shape[:3] + (2 * shape[3],)
-            stride = [2 * s if n > 1 else shape[3] for s, n in zip(stride[:3], shape)] + [1]
+            shape = (shape[0], shape[1], shape[2], 2 * shape[3])
+            stride = (2 * stride[0], 2 * stride[1], 2 * stride[2], 1)
             self._block_scales(k_scale, shape, stride, v_scale)
         else:
             for x in (k_scale, v_scale):
@@ -627,13 +628,15 @@ class PagedCache:
 
     @staticmethod
     def _block_scales(k_scale, shape, stride, v_scale):
-        """Those of element i .. i + 31 lie at i / 32 (pc_kv_cache), so the strides follow from the codes'."""
-        blocks = shape[:3] + (shape[3] // 32,)
+        """Those of elements i .. i + 31 lie at i / 32 (pc_kv_cache), so the strides follow from the codes'."""
+        pages, heads, slots, dim = shape
+        blocks = (pages, heads, slots, dim // 32)
         for x in (k_scale, v_scale):
-            if x.dtype not in (torch.uint8, torch.float8_e8m0fnu) or x.shape != blocks or not x.is_cuda:
+            if (x.dtype is not torch.uint8 and x.dtype is not torch.float8_e8m0fnu) or x.shape != blocks or not x.is_cuda:
                 raise PcError("expected scales %s of float8_e8m0fnu or uint8 on the GPU" % list(blocks))
-            if (blocks[3] > 1 and x.stride(3) != 1) or any(
-                    32 * a != b for a, b, n in zip(x.stride(), stride, shape[:3]) if n > 1):
+            a, b, c, d = x.stride()
+            if ((32 * a != stride[0] and pages > 1) or (32 * b != stride[1] and heads > 1) or
+                    (32 * c != stride[2] and slots > 1) or (d != 1 and dim > 32)):
                 raise PcError("scales: expected a sixteenth of the codes' strides")
 
 
@@ -672,20 +675,21 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str]
     """
     if rot_dim < 2 or rot_dim % 2:
         raise PcError("rot_dim: expected an even number of dimensions")
-    if not (np.isfinite(base) and base > 0 and np.isfinite(factor) and factor > 0):
+    if not (math.isfinite(base) and base > 0 and math.isfinite(factor) and factor > 0):
         raise PcError("base and factor: expected numbers above 0")
     if scaling not in (None, "none", "linear", "base", "ramp"):
         raise PcError("scaling: expected none, linear, base or ramp")
     if scaling == "base" and rot_dim > 2:
         base = base * factor ** (rot_dim / (rot_dim - 2))
-    freq = float(base) ** (np.arange(0, rot_dim, 2, dtype=np.float64) / -rot_dim)
+    freq = float(base) ** (np.arange(0, rot_dim, 2) / -float(rot_dim))
     if scaling == "linear":
         freq = freq / factor
     elif scaling == "ramp":
         if not (trained > 0 and fast > slow):
             raise PcError("ramp: expected the trained length, and slow < fast")
-        keep = np.clip((trained * freq / (2 * np.pi) - slow) / (fast - slow), 0, 1)
-        freq = (1 - keep) * freq / factor + keep * freq
+        keep = (freq * (trained / (2 * math.pi)) - slow) / (fast - slow)
+        keep = np.minimum(np.maximum(keep, 0.0), 1.0)
+        freq = freq * (keep + (1 - keep) / factor)
     return freq
 
 
@@ -698,7 +702,7 @@ def rope_table(freq, n_pos: int, first: int = 0, magnitude: float = 1.0, out: Op
         raise PcError("expected one frequency a pair, and positions below 2^32 - 1")
     shape = (n_pos, freq.size, 2)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=_dev())
+        out = torch.empty(shape, dtype=torch.float32, device="cuda")
     elif out.dtype != torch.float32 or out.shape != shape:
         raise PcError("out: expected %s float32" % list(shape))
     check(L.pc_rope_table(freq.ctypes.data, freq.size, first, n_pos, magnitude, _ptr(out), _stream_of(out)))

@@ -1,8 +1,9 @@
 """pc_rope_table, pc_rope and pc_kv_append_rope against their definitions in 64 bits: layouts, parts
 of heads, types, positions, strides, streams, graphs, refusals.
 
-Bounds.  The angle is the same product in 64 bits on both sides; its reduction and the series are
-off by less than 1e-13, the rounding to 32 bits by 2^-24 of the result.  A turned element is a sum of two
+Bounds.  The angles that a table is compared with are products in 80 bits, off by 2^-64 of themselves; the library's are
+exact, their reduction, the series and the turns from one position to the next off by less than 1e-13 together, the
+rounding to 32 bits by 2^-24 of the result.  A turned element is a sum of two
 products in 32 bits (one rounding of a product, one of the sum: 2^-24 of the sum of their magnitudes each),
 rounded to the type: half a step, u = 2^-9 or 2^-12 of it (2^-25 of a float16 below its normal range);
 twice that is allowed, for a sum that lies next to a border.  Codes of 8 and 4 bits are taken of the exact
@@ -52,10 +53,10 @@ def test_table(pairs, n_pos, first):
     freq = pc.rope_frequencies(2 * pairs, 10000.0, "ramp", 8.0, trained=4096)
     freq[0] = -1.5 if pairs > 1 else 1.0
     got = pc.rope_table(freq, n_pos, first=first, magnitude=1.1).cpu().numpy().astype(np.float64)
-    a = np.multiply.outer(first + np.arange(n_pos, dtype=np.float64), freq)
-    want = 1.1 * np.stack([np.cos(a), np.sin(a)], -1)
+    a = np.multiply.outer(first + np.arange(n_pos, dtype=np.longdouble), freq.astype(np.longdouble))    # 64 bits of fraction
+    want = (1.1 * np.stack([np.cos(a), np.sin(a)], -1)).astype(np.float64)
     assert got.shape == (n_pos, pairs, 2)
-    assert np.all(np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 2e-13)
+    assert np.all(np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 2e-13 + 2.0 ** -63 * np.abs(a.astype(np.float64))[..., None])
 
 
 def test_table_of_nothing_and_refusals():

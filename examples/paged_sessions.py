@@ -1,9 +1,10 @@
 """Sessions over one paged cache: chained block keys find the pages that a prompt
-shares with what is cached, only its other tokens are computed, decode steps
-accumulate the attention weight of every cached token, and sessions that outgrow
-their budget are cut to the tokens with the most of it.
+shares with what is cached, only its other tokens are computed, their queries and keys
+turned by their positions on the way into the cache, decode steps accumulate the
+attention weight of every cached token, and sessions that outgrow their budget are
+cut to the tokens with the most of it.
 
-    python examples/paged_sessions.py [--sessions N] [--steps K] [--budget B]
+    python examples/paged_sessions.py [--sessions N] [--steps K] [--budget B] [--cache bf16|fp4]
 
 One attention layer with random weights stands for a model.
 """
@@ -22,14 +23,21 @@ PAGE = 16
 
 
 class Server:
-    def __init__(self, sessions, heads=8, kv_heads=2, dim=64, n_pages=4096, max_kv=2048, dtype=torch.bfloat16, seed=0):
+    def __init__(self, sessions, heads=8, kv_heads=2, dim=64, n_pages=4096, max_kv=2048, dtype=torch.bfloat16, seed=0,
+                 cache="bf16", positions=8192):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.heads, self.kv_heads, self.dim, self.dtype = heads, kv_heads, dim, dtype
         width = heads * dim
         self.embed = torch.randn(32000, width, generator=g, device="cuda", dtype=dtype)
         self.qkv = torch.randn(width, (heads + 2 * kv_heads) * dim, generator=g, device="cuda", dtype=dtype) * width ** -0.5
-        k = torch.zeros(n_pages, kv_heads, PAGE, dim, device="cuda", dtype=dtype)
-        self.cache = pc.PagedCache(k, torch.zeros_like(k))
+        if cache == "fp4":      # two codes a byte, and the scale of every 32 of them
+            codes, scales = (torch.zeros(2, n_pages, kv_heads, PAGE, n, device="cuda", dtype=torch.uint8) for n in (dim // 2, dim // 32))
+            codes = codes.view(torch.float4_e2m1fn_x2)
+            self.cache = pc.PagedCache(codes[0], codes[1], scales[0], scales[1])
+        else:
+            k = torch.zeros(n_pages, kv_heads, PAGE, dim, device="cuda", dtype=dtype)
+            self.cache = pc.PagedCache(k, torch.zeros_like(k))
+        self.angles = pc.rope_table(pc.rope_frequencies(dim), positions)
         self.free = list(range(n_pages - 1, -1, -1))
         self.users = np.zeros(n_pages, np.int64)      # sessions that hold a page
         self.page_of_key = {}                         # full blocks by their chained key
@@ -37,6 +45,7 @@ class Server:
         self.max_kv = max_kv
         self.pages = [[] for _ in range(sessions)]
         self.len = np.zeros(sessions, np.int64)
+        self.text = np.zeros(sessions, np.int64)      # tokens so far, the evicted ones among them: the next one's position
         self.weight = torch.zeros(sessions, kv_heads, max_kv, device="cuda")
         self.shared_tokens = self.evictions = 0
 
@@ -83,7 +92,7 @@ class Server:
                 self.pages[s].append(page)
             cached = len(self.pages[s]) * PAGE
             self.shared_tokens += cached
-            self.len[s] = cached
+            self.len[s] = self.text[s] = cached
             out.append(self.step([s], [prompt[cached:]])[0])
             for i, key in enumerate(mine):
                 if int(key) not in self.page_of_key:
@@ -94,9 +103,12 @@ class Server:
     def step(self, sessions, tokens):
         """New tokens of some sessions into the cache, and their attention over it."""
         new = np.zeros(len(self.pages), np.int64)
-        for s, t in zip(sessions, tokens):
+        pos = []
+        for s, t in sorted(zip(sessions, tokens), key=lambda x: x[0]):
             new[s] = len(t)
+            pos.append(np.arange(self.text[s], self.text[s] + len(t)))
             self.len[s] += len(t)
+            self.text[s] += len(t)
             while len(self.pages[s]) * PAGE < self.len[s]:
                 self._take(s)
         order = [t for _, t in sorted(zip(sessions, tokens), key=lambda x: x[0])]
@@ -105,7 +117,7 @@ class Server:
         q, k, v = x.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
         # a session that takes no part has no new rows, and keeps its weights
         table, kv_len, q_off = self._table(), self._i32(self.len), self._i32(np.concatenate([[0], np.cumsum(new)]))
-        ws = pc.kv_append(self.cache, table, kv_len, q_off, k, v)
+        q, ws = pc.kv_append_rope(self.cache, table, kv_len, q_off, k, v, self.angles, pos=self._i32(np.concatenate(pos)), q=q, q_out=q)
         out, _, _, ws2 = pc.attn_paged(q, self.cache, table, kv_len, q_off, int(new.max()), max_kv=self.max_kv,
                                        weight=self.weight, weight_out=self.weight)
         for w in (ws, ws2):
@@ -131,9 +143,9 @@ class Server:
         self.evictions += 1
 
 
-def run(sessions=6, steps=40, budget=256, recent=32, seed=0):
+def run(sessions=6, steps=40, budget=256, recent=32, seed=0, cache="bf16"):
     r = np.random.default_rng(seed)
-    server = Server(sessions, seed=seed)
+    server = Server(sessions, seed=seed, cache=cache)
     system = r.integers(0, 32000, 200)
     server.admit([np.concatenate([system, r.integers(0, 32000, int(r.integers(1, 400)))]) for _ in range(sessions)])
     for _ in range(steps):
@@ -149,8 +161,9 @@ def main():
     p.add_argument("--sessions", type=int, default=6)
     p.add_argument("--steps", type=int, default=40)
     p.add_argument("--budget", type=int, default=256)
+    p.add_argument("--cache", choices=["bf16", "fp4"], default="bf16")
     a = p.parse_args()
-    server = run(a.sessions, a.steps, a.budget, min(32, a.budget))
+    server = run(a.sessions, a.steps, a.budget, min(32, a.budget), cache=a.cache)
     print("%d sessions, %d decode steps: %d prompt tokens found in shared pages, %d evictions, lengths %s, %d pages in use" % (
         a.sessions, a.steps, server.shared_tokens, server.evictions, server.len.tolist(), int((server.users > 0).sum())))
 

@@ -569,7 +569,8 @@ pc_status pc_rope_table(const double *freq, uint32_t n_freq, uint64_t first, uin
 /* Rows turned by their positions, in 32 bits and rounded to `dtype` (PC_BF16, PC_F16) once.
  *   x, out    head h of row t at element t * stride_row + h * stride_head, head_dim contiguous
  *             (a multiple of 8, at most PC_MAX_HEAD_DIM); pointers and strides in bytes
- *             multiples of 16.  out may be x, with its strides; else they do not overlap.
+ *             multiples of 16.  out may be x, with its strides; else they do not overlap.  Runs of
+ *             out lie apart (the heads of a row in a block, or the rows of a head).
  *   n_heads   1 .. PC_MAX_HEADS */
 size_t pc_rope_ws(void);
 pc_status pc_rope(const pc_rotation *rotation, const void *x, uint64_t x_stride_row, uint64_t x_stride_head,

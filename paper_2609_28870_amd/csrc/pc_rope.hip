@@ -524,6 +524,13 @@ static pc_status turn_of(const pc_rotation *r, uint32_t dim, uint32_t flags_allo
 }
 static bool aligned(const void *p, uint64_t row, uint64_t head) { return ((uint64_t)(uintptr_t)p | row * 2 | head * 2) % 16 == 0; }
 
+// whether the runs of an array that is written share no memory: the heads of a row in a block, or the rows of a head
+static bool runs_apart(const Entries &x, uint64_t n_rows, uint64_t n_heads, uint64_t width) {
+    if (n_rows < 2 || n_heads < 2) return (n_rows < 2 || x.row >= width) && (n_heads < 2 || x.head >= width);
+    return x.head <= x.row ? x.head >= width && x.row >= (n_heads - 1) * x.head + width
+                           : x.row >= width && x.head >= (n_rows - 1) * x.row + width;
+}
+
 // whether two arrays of rows share memory: the heads of a row in one block each
 static bool rows_overlap(const Entries &x, uint64_t x_bytes, const Entries &y, uint64_t y_bytes, uint64_t n_rows) {
     if (!n_rows || !overlap(x.base, (n_rows - 1) * x.row + x_bytes, y.base, (n_rows - 1) * y.row + y_bytes)) return false;
@@ -580,6 +587,7 @@ pc_status pc_rope(const pc_rotation *rotation, const void *x, uint64_t x_stride_
     const uint32_t cleared = turn.pos && n_rows > ROWS_LOOKED_AT;
     if (!launch_fits(groups + 1, 256)) return PC_ERR_TOO_LARGE;
     if (!ws || ws_bytes < pc_rope_ws()) return PC_ERR_WORKSPACE;
+    if (!runs_apart(to, n_rows, n_heads, 2ull * head_dim)) return PC_ERR_INVALID;
     if (!in_place && entries_overlap(from, to, n_rows, n_heads, 2ull * head_dim)) return PC_ERR_INVALID;
     const hipStream_t st = (hipStream_t)stream;
     if (cleared) {
@@ -622,6 +630,7 @@ pc_status pc_kv_append_rope(const pc_kv_cache *cache, const uint32_t *page_table
         queries = Queries{(const char *)q, (char *)q_out, q_stride_row * 2, q_stride_head * 2, qo_stride_row * 2, qo_stride_head * 2, n_heads};
         const uint64_t run = 2ull * c.kv.dim;
         const Entries from{q, queries.x_row, queries.x_head}, to{q_out, queries.o_row, queries.o_head};
+        if (!runs_apart(to, n_rows, n_heads, run)) return PC_ERR_INVALID;
         if (!(q == q_out && same_strides(from, to, n_rows, n_heads)) && entries_overlap(from, to, n_rows, n_heads, run)) return PC_ERR_INVALID;
         // keys and values are read while queries are written
         const uint64_t q_bytes = (n_heads - 1) * queries.o_head + run;

@@ -281,6 +281,32 @@ def test_a_session_as_it_is_used():
         step(new)
 
 
+def test_weights_of_more_scores_than_are_kept():
+    """Few rows with room for more than 2^30 scores: the weights take a second pass over the keys."""
+    n, kvh, page = 64, 8, 1000
+    r = np.random.default_rng(5)
+    kv = r.integers(1, 300, n)
+    c = Case4(list(kv), [min(4, int(x)) for x in kv], heads=64, kvh=kvh, dim=32, page=page, seed=5, weights=True, cols=66)
+    c.check()
+
+
+def test_the_example_runs_over_4_bits():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_sessions.py")
+    spec = importlib.util.spec_from_file_location("paged_sessions", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    server = example.run(sessions=4, steps=10, budget=96, recent=16, seed=2, cache="fp4")
+    torch.cuda.synchronize()
+    assert server.evictions >= 3 and server.len.max() <= 96 + 4 * 16 + 12 and bool((server.text > server.len).any())
+    q, table, kv_len, q_off, out = server.last
+    k, v = (turn_plain.fp4_values(x, e) for x, e in ((server.cache.k, server.cache.k_scale), (server.cache.v, server.cache.v_scale)))
+    (want, _, _), (tol, _, _) = kv_plain.attention(q, k, v, table.cpu().numpy(), kv_len.cpu().numpy(), q_off.cpu().numpy(),
+                                                   q.shape[2] ** -0.5, True, 0)
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= tol)
+
+
 def test_binding_refuses():
     codes = torch.zeros((4, 2, 16, 32), dtype=torch.uint8, device="cuda")
     e = torch.zeros((4, 2, 16, 2), dtype=torch.uint8, device="cuda")

@@ -71,6 +71,10 @@ def test_rope_rejects(L):   # noqa: F811
     for at in (16, 128, 512, -16, 4 * 512 + 496):
         assert rope(L, out=FAKE + at) == -1                   # over other rows
     assert rope(L, out=FAKE, outr=512) == -1                  # in place, other strides
+    for kw in (dict(outh=0), dict(outr=0), dict(outh=56), dict(outr=248), dict(outr=64, outh=312)):
+        assert rope(L, **kw) == -1                            # results over each other
+    assert rope(L, outr=64, outh=320, ws=None) == -3          # [head, row]
+    assert rope(L, x=FAKE, out=FAKE, xh=0, outh=0) == -1
 
 
 def test_table_rejects(L):   # noqa: F811
@@ -133,6 +137,8 @@ def test_queries_that_overlap(L):   # noqa: F811
     refused(**dict(fused, v=FAKE + 784))
     refused(**dict(fused, kr=1024))
     refused(**dict(fused, oh=128))
+    refused(oh=0)
+    refused(orow=0)
     assert append_rope(L, **dict(fused, ws=None)) == -3       # as they are meant
 
 

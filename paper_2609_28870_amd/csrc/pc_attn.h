@@ -253,7 +253,7 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (ui
 
 // What `key` counts: items; tiles of rows of every head (whatever their ranges); sequences.
 enum class By { ITEM, TILE, SEQ };
-template <By BY>
+template <By BY, bool EVEN = false>   // EVEN: where ranges may be
 __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
     const int lane = threadIdx.x & (WAVE - 1);
     Item it;
@@ -281,7 +281,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
                 if (a.n_seqs > WAVE) h = shape_of(a, s);
                 splits = (h.key_tiles + length - 1) / length;
                 splits = splits ? splits : 1;
-                if (a.even && splits > 1) {
+                if (EVEN && a.even && splits > 1) {
                     length = (h.key_tiles + splits - 1) / splits;
                     splits = (h.key_tiles + length - 1) / length;
                 }
@@ -299,7 +299,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, uint32_t key) {
                 it.there = true;
                 it.seq = s0 + at;
                 it.splits = from_lane(splits, at);
-                it.length = from_lane(length, at);
+                it.length = EVEN ? from_lane(length, at) : longest;
                 it.shape.q.first = from_lane(h.q.first, at);
                 it.shape.q.rows = from_lane(h.q.rows, at);
                 it.shape.q.len = from_lane(h.q.len, at);

@@ -552,7 +552,7 @@ __device__ __forceinline__ float2 join_stats(const AttnArgs &a, const Item &it, 
 // table's entries.  Behind those workgroups, with few rows: the weights, from the scores.
 // Bound by its waits (list, statistics, parts): 6 us for one row, 9 for a decode batch, 19 with the
 // weights of 32 uneven sequences of up to 16,384 slots (45 MB of scores).
-template <class T, int D>
+template <class T, int D, bool EVEN>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t joins, uint32_t row_blocks,
                                                    uint32_t key_blocks) {
     constexpr uint32_t LANES = D / 4, ALL = 256 / LANES;
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
         if (bad) atomicOr(a.status, DEV_ERR_BAD_LAYOUT);
         // join
         const uint32_t tile = blockIdx.x / row_blocks;
-        const Item it = find_item<By::TILE>(a, tile);
+        const Item it = find_item<By::TILE, EVEN>(a, tile);
         if (!it.there || it.splits < 2) return;
         const uint32_t at = tid / LANES, lane = tid % LANES, team = at % teams, step = ALL / teams;
         const uint32_t r0 = it.row_tile * a.row_tile, rows = min(a.row_tile, it.shape.q.rows * a.group - r0);
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
     // weights of WEIGH_KEYS keys of one (sequence, head) from the scores
     const uint32_t b = blockIdx.x - joins, s = b / (key_blocks * a.kv.n_kv), hk = b - s * key_blocks * a.kv.n_kv;
     const uint32_t h = hk / key_blocks, k0 = (hk - h * key_blocks) * WEIGH_KEYS;
-    const Item it = find_item<By::SEQ>(a, s);
+    const Item it = find_item<By::SEQ, EVEN>(a, s);
     const Seq &q = it.shape.q;
     const uint32_t rows = q.rows * a.group;
     const uint32_t r = tid / 8;   // 32 teams of 8
@@ -1021,7 +1021,7 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids 
     } else {
         PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, H, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
     }
-    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D>), dim3((unsigned)(g.joins + g.weigh)), dim3(256), 0, st, a, g.teams, (uint32_t)g.joins,
+    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D, H == Held::E2M1>), dim3((unsigned)(g.joins + g.weigh)), dim3(256), 0, st, a, g.teams, (uint32_t)g.joins,
               g.row_blocks, g.key_blocks);
     if (g.weights) {
         PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, H, D, FULL>), dim3((unsigned)g.weights), dim3(256), 0, st, a, p.key_blocks);

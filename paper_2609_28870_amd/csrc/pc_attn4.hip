@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, rows4_waves(D, R)) void rows4_kernel(AttnArgs 
     __shared__ __attribute__((aligned(16))) char tiles[4 * 32 * D * 2];
     __shared__ float2 join_ml[2][R][64];
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-    const Item it = find_item<By::ITEM>(a, blockIdx.x);
+    const Item it = find_item<By::ITEM, true>(a, blockIdx.x);
     if (!it.there) return;
     const uint32_t lane = threadIdx.x & (WAVE - 1), wave = uniform(threadIdx.x / WAVE), col = lane % 16, quarter = lane / 16;
     const Seq &sq = it.shape.q;

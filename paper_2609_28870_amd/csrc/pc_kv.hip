@@ -489,6 +489,7 @@ constexpr uint32_t MOVE_SLOTS = 64;   // slots of one (sequence, head) per workg
 
 // Keys and values of the kept slots, each a run of 16-byte pieces: bound by memory.  (Pieces
 // looked up and loaded four at a time took 100 us for what this does in 84, and 9 for 4.)
+template <bool F4>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t groups) {
     const uint32_t row = blockIdx.x / groups, r0 = (blockIdx.x - row * groups) * MOVE_SLOTS;
     const uint32_t s = row / a.kv.n_kv, h = row - s * a.kv.n_kv;
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, uint32_t g
         const uint4 x = *(const uint4 *)(a.kv.k + src), y = *(const uint4 *)(a.kv.v + src);
         *(uint4 *)(a.kv.k + dst) = x;
         *(uint4 *)(a.kv.v + dst) = y;
-        if (a.kv.k_exp) {   // 16 bytes of 4-bit codes are a block
+        if (F4) {   // 16 bytes of codes are a block
             a.kv.k_exp[dst / 16] = a.kv.k_exp[src / 16];
             a.kv.v_exp[dst / 16] = a.kv.v_exp[src / 16];
         }
@@ -649,7 +650,10 @@ pc_status pc_kv_evict(const pc_kv_cache *cache, const uint32_t *page_table, uint
     } else {
         PC_LAUNCH(K_KV_EVICT_SELECT, evict_select_kernel, dim3(rows), dim3(SELECT_THREADS), 0, st, a);
     }
-    if (dst_table) PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel, dim3(rows * groups), dim3(256), 0, st, a, groups);
+    if (dst_table) {
+        if (a.kv.k_exp) PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel<true>, dim3(rows * groups), dim3(256), 0, st, a, groups);
+        else PC_LAUNCH(K_KV_EVICT_MOVE, evict_move_kernel<false>, dim3(rows * groups), dim3(256), 0, st, a, groups);
+    }
     return PC_OK;
 }
 

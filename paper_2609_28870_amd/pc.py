@@ -621,9 +621,12 @@ class PagedCache:
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
         if 1 in shape:   # the stride of a dimension of one is anything
             stride = [s if n > 1 else self.head_dim for s, n in zip(stride, shape)]
-        scales = [x.data_ptr() for x in (k_scale, v_scale)] if dtype == 3 else [_ptr(k_scale), _ptr(v_scale)]
-        self._c = _KvCache(k.data_ptr(), v.data_ptr(), *scales, stride[0], stride[1], stride[2], dtype,
-                           self.n_pages, self.page_size, self.n_kv_heads, self.head_dim)
+        if dtype == 3:
+            ka, va = k_scale.data_ptr(), v_scale.data_ptr()
+        else:
+            ka, va = _ptr(k_scale), _ptr(v_scale)
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), ka, va, stride[0], stride[1], stride[2], dtype, self.n_pages,
+                           self.page_size, self.n_kv_heads, self.head_dim)
         self._at = ctypes.addressof(self._c)
 
     @staticmethod

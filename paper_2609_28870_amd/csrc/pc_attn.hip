@@ -550,9 +550,9 @@ __device__ __forceinline__ float2 join_stats(const AttnArgs &a, const Item &it, 
 // The parts of some rows of a tile, `teams` of D / 4 lanes to a row, each over every
 // teams-th part; and the whole call's status, for which the workgroups share the
 // table's entries.  Behind those workgroups, with few rows: the weights, from the scores.
-// Bound by its waits (list, statistics, parts): 6 us for one row, 9 for a decode batch, 19 with the
-// weights of 32 uneven sequences of up to 16,384 slots (45 MB of scores).
-template <class T, int D, bool EVEN>
+// Bound by its waits (list, statistics, parts): 6 us for one row, 8 for a decode batch; with the weights of
+// 64 uneven sequences of up to 32,768 slots (79 MB of scores read, 43 MB of weights read and written) 32.
+template <class T, int D, bool EVEN, bool WEIGH>   // WEIGH: the launch has workgroups for weights
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, uint32_t joins, uint32_t row_blocks,
                                                    uint32_t key_blocks) {
     constexpr uint32_t LANES = D / 4, ALL = 256 / LANES;
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
     __shared__ float stats[32];
     __shared__ int2 sees[32];   // first and last slot
     const uint32_t tid = threadIdx.x;
-    if (blockIdx.x < joins) {
+    if (!WEIGH || blockIdx.x < joins) {
         // status
         bool bad = false;
         if (blockIdx.x == 0 && tid == 0) bad = a.q_off[0] != 0 || a.q_off[a.n_seqs] != a.n_rows;
@@ -651,45 +651,78 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, uint32_t teams, u
         }
         return;
     }
+    if constexpr (!WEIGH) return;
     // weights of WEIGH_KEYS keys of one (sequence, head) from the scores
     const uint32_t b = blockIdx.x - joins, s = b / (key_blocks * a.kv.n_kv), hk = b - s * key_blocks * a.kv.n_kv;
-    const uint32_t h = hk / key_blocks, k0 = (hk - h * key_blocks) * WEIGH_KEYS;
-    const Item it = find_item<By::SEQ, EVEN>(a, s);
-    const Seq &q = it.shape.q;
+    const uint32_t h = hk / key_blocks;
+    // Neighbouring workgroups are on different XCDs, and the first keys are there in every sequence: each row begins
+    // one block later, so that no XCD gets the same blocks of all of them (64 sequences with room for
+    // 32,768 slots, a multiple of eight blocks: 48 us, rotated 32).
+    const uint32_t block = (hk - h * key_blocks + s * a.kv.n_kv + h) % key_blocks, k0 = block * WEIGH_KEYS;
+    const Shape shape = shape_of(a, s);
+    const Seq &q = shape.q;
     const uint32_t rows = q.rows * a.group;
-    const uint32_t r = tid / 8;   // 32 teams of 8
-    if (r < rows) {
-        const uint32_t i = a.by_group.div(r);
-        float base2;
-        if (it.splits > 1) {
-            const float2 ml = join_stats(a, it, h, 0, r, tid % 8, 8);
-            base2 = log_sum<T>(ml.x, ml.y);
-        } else {
-            base2 = a.lse2[(uint64_t)(q.first + i) * a.n_heads + h * a.group + (r - i * a.group)];
-        }
-        if (tid % 8 == 0) {
-            stats[r] = base2 == MINUS_INF ? __builtin_inff() : base2;   // a row without a weight: exp2(-inf)
-            seen_by_row(a, q, i, &sees[r].x, &sees[r].y);
-        }
-    }
-    __syncthreads();
+    // four keys a thread, so that a row's scores are one load (rows of them begin at multiples of 32)
+    static_assert(WEIGH_KEYS == 4 * 256, "four keys a thread");
     const uint64_t row = (uint64_t)s * a.kv.n_kv + h;
-    for (uint32_t j = k0 + tid; j < min(k0 + WEIGH_KEYS, a.max_kv); j += 256) {
-        float w = 0.f;
-        if (j < q.len) {
-            w = a.weight ? a.weight[row * a.weight_stride + j] : 0.f;
-            if (j >= it.shape.keys.lo && j < it.shape.keys.hi) {
-                const float *x = a.scores + row * a.slot_rows * a.score_stride + j;
-                float sum = 0.f;
-#pragma unroll 8
-                for (uint32_t i = 0; i < rows; ++i) {
-                    const float e = exp2_fast(x[i * a.score_stride] - stats[i]);   // NaN of a broken row: for what it sees
-                    sum += (((int32_t)j >= sees[i].x) & ((int32_t)j <= sees[i].y)) ? e : 0.f;
-                }
-                w += sum;
+    const uint32_t j = k0 + 4 * tid, end = min(a.max_kv, q.len);
+    float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const uint64_t at = row * a.weight_stride + j;
+    const bool pieces = ((uint64_t)(uintptr_t)a.weight_out | (uint64_t)(uintptr_t)a.weight | a.weight_stride * 4) % 16 == 0;
+    if (a.weight && pieces && j + 4 <= end) {
+        const float4 w = *(const float4 *)(a.weight + at);
+        old[0] = w.x, old[1] = w.y, old[2] = w.z, old[3] = w.w;
+    } else {
+#pragma unroll
+        for (uint32_t n = 0; n < 4; ++n) old[n] = a.weight && j + n < end ? a.weight[at + n] : 0.f;
+    }
+    if (k0 < shape.keys.hi && k0 + WEIGH_KEYS > shape.keys.lo) {   // else no row sees any of them
+        const bool scored = j < shape.keys.hi && j + 4 > shape.keys.lo;
+        const float *x = a.scores + row * a.slot_rows * a.score_stride + (scored ? j : shape.keys.lo);
+        // the first rows' scores are on their way while the statistics are found
+        constexpr uint32_t FIRST = 8;
+        float4 z[FIRST];
+#pragma unroll
+        for (uint32_t i = 0; i < FIRST; ++i) z[i] = *(const float4 *)(x + min(i, rows - 1) * a.score_stride);
+        const Item it = find_item<By::SEQ, EVEN>(a, s);
+        const uint32_t r = tid / 8;   // 32 teams of 8
+        if (r < rows) {
+            const uint32_t i = a.by_group.div(r);
+            float base2;
+            if (it.splits > 1) {
+                const float2 ml = join_stats(a, it, h, 0, r, tid % 8, 8);
+                base2 = log_sum<T>(ml.x, ml.y);
+            } else {
+                base2 = a.lse2[(uint64_t)(q.first + i) * a.n_heads + h * a.group + (r - i * a.group)];
+            }
+            if (tid % 8 == 0) {
+                stats[r] = base2 == MINUS_INF ? __builtin_inff() : base2;   // a row without a weight: exp2(-inf)
+                seen_by_row(a, q, i, &sees[r].x, &sees[r].y);
             }
         }
-        a.weight_out[row * a.weight_stride + j] = w;
+        __syncthreads();
+        auto add = [&](uint32_t i, float4 z) {
+            const float y[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) {
+                const float e = exp2_fast(y[n] - stats[i]);   // NaN of a broken row: for what it sees
+                sum[n] += (((int32_t)(j + n) >= sees[i].x) & ((int32_t)(j + n) <= sees[i].y)) ? e : 0.f;
+            }
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < FIRST; ++i)
+            if (i < rows) add(i, z[i]);
+#pragma unroll 8
+        for (uint32_t i = FIRST; i < rows; ++i) add(i, *(const float4 *)(x + i * a.score_stride));
+    }
+#pragma unroll
+    for (uint32_t n = 0; n < 4; ++n) sum[n] = j + n < end ? old[n] + sum[n] : 0.f;
+    if (pieces && j + 4 <= a.max_kv) {
+        *(float4 *)(a.weight_out + at) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    } else {
+#pragma unroll
+        for (uint32_t n = 0; n < 4; ++n)
+            if (j + n < a.max_kv) a.weight_out[at + n] = sum[n];
     }
 }
 
@@ -1021,8 +1054,14 @@ static pc_status attn_run(const AttnArgs &a, const AttnPlan &p, const AttnGrids 
     } else {
         PC_LAUNCH(K_ATTN_CHUNK, (chunk_kernel<T, H, D, FULL, CHUNK_WAVES>), items, dim3(CHUNK_WAVES * WAVE), 0, st, a);
     }
-    PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D, H == Held::E2M1>), dim3((unsigned)(g.joins + g.weigh)), dim3(256), 0, st, a, g.teams, (uint32_t)g.joins,
-              g.row_blocks, g.key_blocks);
+    const dim3 joins((unsigned)(g.joins + g.weigh));
+    constexpr bool EVEN = H == Held::E2M1;
+    if (g.weigh)
+        PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D, EVEN, true>), joins, dim3(256), 0, st, a, g.teams, (uint32_t)g.joins, g.row_blocks,
+                  g.key_blocks);
+    else
+        PC_LAUNCH(K_ATTN_JOIN, (join_kernel<T, D, EVEN, false>), joins, dim3(256), 0, st, a, g.teams, (uint32_t)g.joins, g.row_blocks,
+                  g.key_blocks);
     if (g.weights) {
         PC_LAUNCH(K_ATTN_WEIGHT, (weight_kernel<T, H, D, FULL>), dim3((unsigned)g.weights), dim3(256), 0, st, a, p.key_blocks);
         if (p.weight_parts > 1) PC_LAUNCH(K_ATTN_WEIGHT, weight_sum_kernel, dim3((unsigned)g.sums), dim3(256), 0, st, a, p.key_blocks);

@@ -215,7 +215,8 @@ __device__ __forceinline__ bool positions_bad(const uint32_t *__restrict__ pos, 
     return most >= n_pos;
 }
 
-// A read and a write of the rows, the angles from a cache: bound by memory.
+// A read and a write of the rows, the angles from a cache: bound by memory (16,384 rows of 32 heads of 128,
+// 271 MB: 44 us in passes that follow each other; one head a thread instead of four took 52).
 template <bool BF, Layout L>
 __global__ __launch_bounds__(256) void rope_kernel(Queries q, Turn turn, Shape g, uint32_t n_rows, int32_t *status, uint32_t cleared) {
     const uint32_t block = cleared ? blockIdx.x : blockIdx.x - 1;
@@ -359,7 +360,8 @@ __device__ __forceinline__ uint4 to_e2m1(const float (&y)[32], uint32_t *exponen
 
 // One launch: a workgroup for the status word, then keys and values, a 16-byte piece of the
 // cache a thread, then queries.  CACHE: PC_FP8_E4M3, PC_FP4_E2M1, or the new tokens' own type.
-// Bound by memory, or for a few tokens by the launch and the chain of loads to a row's page.
+// Bound by memory, or for a few tokens by the launch and the chain of loads to a row's page: 268 MB of
+// ragged chunks into 4 bits 58 us (4.6 TB/s), into 8 bits 62; 256 single tokens 5 us.
 template <bool BF, Layout L, uint32_t CACHE>
 __global__ __launch_bounds__(256) void append_turned_kernel(AppendTurnedArgs a) {
     __shared__ uint64_t to[GROUP_ROWS];

@@ -583,7 +583,8 @@ pc_status pc_rope(const pc_rotation *rotation, const void *x, uint64_t x_stride_
  *   rotation  not PC_ROPE_TRANSPOSE
  *   q, q_out  rows like k, n_heads heads of them, and what pc_rope makes of them; both NULL:
  *             none.  q_out may be q, with its strides; else they do not overlap, and q_out
- *             shares no memory with k and v (rows of one stride may lie beside each other's).
+ *             shares no memory with k and v (rows of one stride may lie beside each other's, and heads
+ *             of one stride between each other's).
  * A row left out for its position, or that has no slot where positions are slots, leaves q_out
  * untouched, too. */
 size_t pc_kv_append_rope_ws(void);

@@ -535,13 +535,20 @@ static bool runs_apart(const Entries &x, uint64_t n_rows, uint64_t n_heads, uint
                            : x.row >= width && x.head >= (n_rows - 1) * x.row + width;
 }
 
-// whether two arrays of rows share memory: the heads of a row in one block each
-static bool rows_overlap(const Entries &x, uint64_t x_bytes, const Entries &y, uint64_t y_bytes, uint64_t n_rows) {
+// Whether two arrays of rows may share memory, the one of x_heads, the other of y_heads heads: known not to where the
+// heads of a row make a block each and the blocks lie apart, or where heads of one stride lie in each other's gaps (each
+// head's query, key and value beside each other), which more heads than there are cannot change.
+static bool rows_overlap(Entries x, uint64_t x_heads, Entries y, uint64_t y_heads, uint64_t n_rows, uint64_t width) {
+    const uint64_t x_bytes = (x_heads - 1) * x.head + width, y_bytes = (y_heads - 1) * y.head + width;
     if (!n_rows || !overlap(x.base, (n_rows - 1) * x.row + x_bytes, y.base, (n_rows - 1) * y.row + y_bytes)) return false;
-    if (n_rows < 2 || x.row != y.row || !x.row) return true;
-    const uint64_t apart = (uint64_t)(uintptr_t)y.base - (uint64_t)(uintptr_t)x.base, back = 0 - apart;
-    const uint64_t d = (int64_t)apart < 0 ? (x.row - back % x.row) % x.row : apart % x.row;
-    return d < x_bytes || d + y_bytes > x.row;
+    if (n_rows > 1 && x.row == y.row && x.row) {
+        const uint64_t apart = (uint64_t)(uintptr_t)y.base - (uint64_t)(uintptr_t)x.base, back = 0 - apart;
+        const uint64_t d = (int64_t)apart < 0 ? (x.row - back % x.row) % x.row : apart % x.row;
+        if (d >= x_bytes && d + y_bytes <= x.row) return false;
+    }
+    if (x_heads < 2) x.head = y.head;   // the stride of one head is anything
+    if (y_heads < 2) y.head = x.head;
+    return entries_overlap(x, y, n_rows, x_heads < y_heads ? y_heads : x_heads, width);
 }
 
 }  // namespace pc
@@ -637,9 +644,8 @@ pc_status pc_kv_append_rope(const pc_kv_cache *cache, const uint32_t *page_table
         if (!runs_apart(to, n_rows, n_heads, run)) return PC_ERR_INVALID;
         if (!(q == q_out && same_strides(from, to, n_rows, n_heads)) && entries_overlap(from, to, n_rows, n_heads, run)) return PC_ERR_INVALID;
         // keys and values are read while queries are written
-        const uint64_t q_bytes = (n_heads - 1) * queries.o_head + run;
-        if (rows_overlap(to, q_bytes, Entries{k, k_stride_row * 2, 0}, (c.kv.n_kv - 1) * k_stride_head * 2 + run, n_rows) ||
-            rows_overlap(to, q_bytes, Entries{v, v_stride_row * 2, 0}, (c.kv.n_kv - 1) * v_stride_head * 2 + run, n_rows))
+        if (rows_overlap(to, n_heads, Entries{k, k_stride_row * 2, k_stride_head * 2}, c.kv.n_kv, n_rows, run) ||
+            rows_overlap(to, n_heads, Entries{v, v_stride_row * 2, v_stride_head * 2}, c.kv.n_kv, n_rows, run))
             return PC_ERR_INVALID;
     }
     if (!ws || ws_bytes < pc_kv_append_rope_ws()) return PC_ERR_WORKSPACE;

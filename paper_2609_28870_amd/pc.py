@@ -528,7 +528,9 @@ def belady(nxt: torch.Tensor, caps: torch.Tensor, depth: Optional[torch.Tensor] 
 # ------------------------------------------------------------- paged cache
 
 # PC_BF16, PC_F16, PC_FP8_E4M3, PC_FP4_E2M1
-_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, torch.float4_e2m1fn_x2: 3}
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+if hasattr(torch, "float4_e2m1fn_x2"):   # newer than the other types: without it there are no caches in 4 bits
+    _DTYPES[torch.float4_e2m1fn_x2] = 3
 _INTS = (torch.int32, torch.uint32)
 _MAX_KV = 0x7FFF0000
 

@@ -684,17 +684,21 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str]
         raise PcError("base and factor: expected numbers above 0")
     if scaling not in (None, "none", "linear", "base", "ramp"):
         raise PcError("scaling: expected none, linear, base or ramp")
-    if scaling == "base" and rot_dim > 2:
-        base = base * factor ** (rot_dim / (rot_dim - 2))
-    freq = float(base) ** (np.arange(0, rot_dim, 2) / -float(rot_dim))
-    if scaling == "linear":
-        freq = freq / factor
-    elif scaling == "ramp":
-        if not (trained > 0 and fast > slow):
-            raise PcError("ramp: expected the trained length, and slow < fast")
-        keep = (freq * (trained / (2 * math.pi)) - slow) / (fast - slow)
-        keep = np.minimum(np.maximum(keep, 0.0), 1.0)
-        freq = freq * (keep + (1 - keep) / factor)
+    base = np.float64(base)
+    with np.errstate(over="ignore", invalid="ignore"):
+        if scaling == "base" and rot_dim > 2:
+            base = base * np.float64(factor) ** (rot_dim / (rot_dim - 2))
+        freq = base ** (np.arange(0, rot_dim, 2) / -float(rot_dim))
+        if scaling == "linear":
+            freq = freq / factor
+        elif scaling == "ramp":
+            if not (trained > 0 and fast > slow):
+                raise PcError("ramp: expected the trained length, and slow < fast")
+            keep = (freq * (trained / (2 * math.pi)) - slow) / (fast - slow)
+            keep = np.minimum(np.maximum(keep, 0.0), 1.0)
+            freq = freq * (keep + (1 - keep) / factor)
+    if not (np.isfinite(base) and np.isfinite(freq).all()):
+        raise PcError("base, factor or ramp: the angles are past what 64 bits hold")
     return freq
 
 

@@ -492,7 +492,9 @@ pc_status pc_belady(const uint32_t *next, const uint32_t *depth, uint64_t n, con
  *               i / 2), whose values are the codes times 2^(b - 127), b the scale
  *               byte of their 32 elements (255: NaN): that of elements i .. i + 31, i a
  *               multiple of 32, is byte i / 32 of k_scale (v_scale), which the calls that
- *               write k (v) write, too.  Queries of PC_F16 read it rounded to their type.
+ *               write k (v) write, too, though they are declared const (for the scales per
+ *               head, which are only read).  Queries of PC_F16 read the values rounded to their
+ *               type: infinite from 65520 in magnitude on, 0 up to 2^-25.
  *   head_dim    a multiple of 16 (PC_FP4_E2M1: of 32), at most PC_MAX_HEAD_DIM
  *   k, v and the strides in bytes are multiples of 16
  *
@@ -546,9 +548,10 @@ pc_status pc_kv_append(const pc_kv_cache *cache, const uint32_t *page_table, uin
  * of x, and undoes the rotation where c^2 + s^2 = 1.
  *
  *   table    float[n_pos][rot_dim / 2][2], a multiple of 8 bytes
- *   pos      uint32[n_rows]: the position of every row; NULL: pc_rope, row t is at position t;
- *            pc_kv_append_rope, at its slot.  Rows whose position is n_pos or more are left out
- *            (status 2).
+ *   pos      uint32[n_rows]: the position of every row; NULL: pc_rope, row t is at position t
+ *            (n_rows above n_pos is PC_ERR_INVALID); pc_kv_append_rope, at its slot.  Rows whose
+ *            position is n_pos or more are left out (status 2).
+ *   n_pos    1 .. 2^32 - 2
  *   rot_dim  even, 2 .. head_dim
  * ------------------------------------------------------------------------ */
 typedef struct {
@@ -579,7 +582,7 @@ pc_status pc_rope(const pc_rotation *rotation, const void *x, uint64_t x_stride_
 
 /* pc_kv_append of keys that are turned on the way (values are not), and in the same launch the
  * new tokens' queries.  A cache of the rows' type holds what pc_rope gives; codes of 8 and 4 bits
- * are taken of the turned value rounded to 32 bits, the sum of its two exact products.
+ * are taken of the sum of the two exact products in 64 bits, rounded to 32.
  *   rotation  not PC_ROPE_TRANSPOSE
  *   q, q_out  rows like k, n_heads heads of them, and what pc_rope makes of them; both NULL:
  *             none.  q_out may be q, with its strides; else they do not overlap, and q_out

@@ -33,10 +33,10 @@ __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
     return make_uint4(pack2<BF>(f[0], f[1]), pack2<BF>(f[2], f[3]), pack2<BF>(f[4], f[5]), pack2<BF>(f[6], f[7]));
 }
 
-// x c + y s.  For 16-bit results 32 bits are enough (two roundings of 2^-24 before one of 2^-9 or
-// 2^-12).  Codes of 8 and 4 bits take the exact sum rounded to 32 bits once (a product of a
-// 16-bit and a 32-bit number is exact in 64): what is next to a border between two codes is then
-// on the same side for whoever computes it.
+// x c + y s.  For 16-bit results 32 bits are enough (two roundings of 2^-24 before one of 2^-8 or
+// 2^-11).  Codes of 8 and 4 bits take the sum in 64 bits, rounded to 32 (a product of a
+// 16-bit and a 32-bit number is exact in 64, so the sum has one rounding there): what is next to a border between two
+// codes is then on the same side for whoever computes it in 64 bits.
 template <bool EXACT>
 __device__ __forceinline__ float turned(float x, float y, float c, float s) {
     if (EXACT) return (float)fma((double)x, (double)c, (double)y * (double)s);
@@ -56,8 +56,9 @@ struct Frequencies {
 };
 
 // Cosine and sine of the product p f, p a whole number below 2^32: the product and what its rounding
-// leaves, less a multiple of pi/2 (exact in the fused sums), then their series on
-// |r| <= pi/4 up to r^14 and r^13, off by less than 3e-14.
+// leaves, less a multiple of pi/2 (exact in the fused sums), then their series up to r^14 and
+// r^13.  |r| is at most pi/4, but for large products: near 2^48, the largest, their own rounding and the
+// quotient's add up to 0.08.  The first terms left out are r^15 / 15! and r^16 / 16!: 2.1e-14 at pi/4, 1e-13 at 0.87.
 __device__ __forceinline__ double2 turn_by(double p, double f) {
     const double a = p * f, n = rint(a * TWO_OVER_PI);
     const double r = fma(-n, HALF_PI, a) + fma(-n, HALF_PI_REST, fma(p, f, -a)), z = r * r;

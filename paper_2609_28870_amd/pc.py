@@ -677,6 +677,9 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str]
     "ramp"    by parts (Peng et al. 2023): a pair that makes t = ``trained`` f_i / (2 pi) turns over the context that was
               trained keeps its f_i where t >= fast, takes f_i / factor where t <= slow, and in between
               (1 - g) f_i / factor + g f_i with g = (t - slow) / (fast - slow).
+    A checkpoint whose ramp runs otherwise, such as over i between two bounds rounded to whole numbers, needs
+    frequencies of its own: ``rope_table`` takes any array.  The ramp's paper scales queries and keys, too, so that
+    their products grow with the context: ``rope_table(magnitude=0.1 * math.log(factor) + 1)``.
     """
     if rot_dim < 2 or rot_dim % 2:
         raise PcError("rot_dim: expected an even number of dimensions")

@@ -134,3 +134,20 @@ def test_appends_past_32_bits(cache):
         for p, s, slot in ((pages - 1, 1, 1023), (pages - 2, 0, 0)):
             got, want = x[p, :, slot].view(torch.uint8), y[s, :, slot].view(torch.uint8)
             assert torch.equal(got, want) and bool(want.any())
+
+
+def test_codes_are_of_the_sum_in_64_bits_rounded_to_32():
+    """3 c is halfway between 5, itself halfway between the codes 4 and 6, and the next number of 32 bits.  The
+    other product moves the exact sum off that half: past 2^-52 of it 64 bits hold that, below they do not."""
+    c = 6990507 * 2.0 ** -22
+    assert float(torch.tensor(c)) == c and 3 * 6990507 == 5 * 2 ** 22 + 1
+    for small, code in ((2.0 ** -40, 7), (-(2.0 ** -40), 6), (2.0 ** -60, 6), (-(2.0 ** -60), 6), (0.0, 6)):
+        table = torch.tensor([[[c, -small]]], dtype=torch.float32).cuda()
+        k = torch.zeros((1, 1, 32), dtype=BF16)
+        k[0, 0, 0], k[0, 0, 1], k[0, 0, 31] = 3.0, 1.0, 6.0
+        codes = torch.zeros((2, 1, 1, 1, 16), dtype=torch.uint8, device="cuda")
+        e = torch.zeros((2, 1, 1, 1, 1), dtype=torch.uint8, device="cuda")
+        _, ws = pc.kv_append_rope(pc.PagedCache(codes[0].view(FP4), codes[1].view(FP4), e[0], e[1]), i32([[0]]), i32([1]), i32([0, 1]),
+                                  k.cuda(), k.cuda(), table)
+        assert pc.workspace_status(ws) == 0
+        assert int(e[0]) == 127 and int(codes[0, 0, 0, 0, 0]) & 15 == code

@@ -1152,7 +1152,10 @@ pc_status pc_attn_paged(const pc_kv_cache *cache, const uint32_t *page_table, ui
     a.cut_first = p.ragged;   // few rows: items are alike but for the last (drafted tokens 28 us, cut first 31)
     a.even = cache->dtype == PC_FP4_E2M1 && p.few;
     if (a.even) {
-        // one round of the chip, less the half range more that every sequence and head is likely to make
+        // One round of the chip, less the half range more that every uneven sequence and head is likely to make (618k
+        // keys in 63 of them 139 -> 82 us).  Even ones make none or a whole one, and where they all make one the second
+        // round is mostly empty: 32,768 keys over 4 heads of 128 for 16 / 20 / 24 / 28 / 32 sequences 61 / 99 / 94 / 140 /
+        // 125 us.
         const uint32_t round = rows4_resident(p.dim, p.slot_rows), halves = (uint32_t)((uint64_t)n_seqs * a.kv.n_kv / 2 < round / 2
                                                                                            ? n_seqs * a.kv.n_kv / 2 : round / 2);
         a.target = round - halves;

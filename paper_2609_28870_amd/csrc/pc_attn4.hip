@@ -94,7 +94,8 @@ constexpr __host__ __device__ uint32_t rows4_waves(uint32_t dim, uint32_t tiles)
 // heads pays for 16, not 32; queries stay in registers, keys are widened straight into them,
 // values pass through LDS for the transposed read.
 // Where 16 slots share a page (by_16) a table entry is read for 16 keys, 32 tiles ahead, and
-// the address is one number for the wave.
+// the address is one number for the wave; else every lane looks its key's up (63 uneven sequences: pages of 16, 24 and 64
+// slots 88 to 90 us, of one slot 207).
 // Bound by memory: 32 over 4 heads of 128, 1.05M keys in 8 even sequences (570 MB) 106 us, 5.4 TB/s; 618k in 63
 // uneven ones 70 us, 4.8 TB/s (two tiles on their way instead of one: 2% slower, with 160 registers for
 // 138); one token over 1,537 keys 9 us, a chain of dependent loads.

@@ -112,7 +112,9 @@ __global__ __launch_bounds__(256) void rope_table_kernel(Frequencies freq, uint3
 // Where a workgroup's threads are: a unit is what one thread turns of one head (eight dimensions
 // and their partners, or one and its partner in layouts of any size), then the pieces
 // that stay as they are.  A thread takes the same unit of every `apart`-th head, so that
-// it reads its cosines once.
+// it reads its cosines once.  Halves of a part that is no multiple of 16 (Layout::ANY) go two bytes at a time,
+// what does not turn among them: 16,384 rows of 20 heads of 96, 24 turned 76 us (in place, where only those move, 13),
+// 32 turned 31 (14).
 struct Shape {
     uint32_t units, turning;   // of a head; of them, those that turn
     uint32_t apart;            // threads to a unit of a row
